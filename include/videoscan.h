@@ -430,6 +430,103 @@ vs_status vs_frame_decoder_layer(const vs_shape *shape, const vs_layer_weights *
                                  const void *h_in, int32_t n_tokens, void *h_out, void *workspace,
                                  size_t workspace_bytes, void *hip_stream);
 
+/*
+ * Rotary positions with several axes, for the rows of Q and K between their projection and the attention (the paper's
+ * statement applies none; the backbone it is built on does).  Of a head's head_dim values the first 2 n are n pairs,
+ * n = sections[0] + sections[1] + sections[2]; the first sections[0] pairs turn with the token's position in time, the next
+ * sections[1] with its height, the last sections[2] with its width:
+ *   pair i: angle = positions[axis of i][token] * theta^(-i / n),  (a, b) -> (a cos - b sin, a sin + b cos)
+ * VS_ROTARY_HALVES: pair i is values i and i + n; VS_ROTARY_ADJACENT: values 2 i and 2 i + 1.  Values behind the first 2 n stay as
+ * they are.  One axis: its section n, the others 0.  Angles are reduced in fp64 (positions may be anything that an int32
+ * holds), the rotation is fp32, each value is rounded once.
+ */
+typedef enum { VS_ROTARY_HALVES = 0, VS_ROTARY_ADJACENT = 1 } vs_rotary_pairing;
+
+/* Made once, kept by the caller (host memory). */
+typedef struct {
+    int32_t head_dim;
+    int32_t sections[3];
+    int32_t pairing;  /* vs_rotary_pairing */
+    int32_t reserved;
+    double turns[64]; /* revolutions of pair i per position: theta^(-i / n) / (2 pi); may be replaced, e.g. for stretched positions */
+} vs_rotary_plan;
+
+/* head_dim 64 or 128; sections of at least 0 whose sum is a multiple of 8, 8 .. head_dim / 2; theta > 0.  Host work only. */
+vs_status vs_rotary_plan_make(int32_t head_dim, const int32_t *sections, double theta, int32_t pairing, vs_rotary_plan *plan);
+
+/*
+ * q, q_out [n_tokens][n_q_heads][head_dim], k, k_out [n_tokens][n_kv_heads][head_dim], positions int32 [3][n_tokens], all
+ * device memory (positions 4-byte aligned).  q or k may be NULL, with its output.  An output may be its input (rows turned in place);
+ * any other overlap of the two is refused (VS_ERR_SHAPE).  inverse != 0 turns back: the gradient of the rotation with
+ * respect to its input, and the way to give kept rows other positions.  1 <= n_tokens <= 2^26.  No workspace.
+ */
+vs_status vs_rotary(const vs_shape *shape, const vs_rotary_plan *plan, const int32_t *positions, int32_t n_tokens, const void *q,
+                    const void *k, int32_t inverse, void *q_out, void *k_out, void *hip_stream);
+
+/*
+ * Retained rows in 8 bits: the same caches at 51 % of the bytes.  A row x of 128 values (of one token and KV head; K and V apart)
+ * is held as whole numbers r_j = rint(x_j / s), ties to even, -127 .. 127, and a scale s = max(ceil8(max_j |x_j| / 127), 2^-126),
+ * where ceil8 goes up to the next number of 8 significant bits (a bf16).  It stands for r_j * s.  Every row is rounded once,
+ * when it is written, by itself: len may be lowered to any number of rows and the cache grown again from there.  A row with
+ * a value that is not finite stands for NaN in all its values.  bf16 shapes only (VS_ERR_UNSUPPORTED otherwise).
+ *
+ * A cache of `capacity` rows is vs_cache8_bytes(shape, capacity) bytes of device memory, 16-byte aligned (0: the shape is not
+ * supported, or capacity < 1 or beyond 1 TiB).  It needs no preparation.  What lies in it is the library's business but for this: it begins with
+ * the same bytes whatever the capacity, so the first vs_cache8_bytes(shape, len) bytes are a copy of the len rows.
+ * Several caches of one capacity lie behind one another (a slab).
+ */
+typedef struct {
+    void *data;       /* device, vs_cache8_bytes(shape, capacity) */
+    int32_t capacity; /* rows there is room for */
+    int32_t len;      /* rows valid, host-side truth */
+} vs_cache8;
+
+size_t vs_cache8_bytes(const vs_shape *shape, int32_t capacity);
+
+/* Bytes of workspace for vs_cache8_prefill_attn with up to max_q_tokens tokens over up to max_cache_rows rows, and for
+ * vs_cache8_decode_attn with up to n_streams streams (0 of either: not used for that call).  Prepared with vs_workspace_init. */
+size_t vs_cache8_workspace_bytes(const vs_shape *shape, int32_t max_q_tokens, int32_t max_cache_rows, int32_t n_streams);
+
+/*
+ * Rows quantised as they are written.  slab: n_caches caches; k_rows, v_rows [n_caches][n_tokens][n_kv_heads][head_dim] (bf16):
+ * for every i, rows first_kept .. n_tokens - 1 go behind the lens[i] rows of cache i (n_tokens - 1: a frame's carrier; 0: all,
+ * as a question's rows or a whole cache in bf16) and lens[i] grows by their number.  If any cache has no room nothing is
+ * done (VS_ERR_CAPACITY).  1 <= n_caches <= 2^20, launched in groups of 64; after a VS_ERR_HIP lens has advanced for exactly
+ * the groups that were enqueued.
+ */
+vs_status vs_cache8_append(const vs_shape *shape, int32_t n_caches, void *slab, int32_t capacity, int32_t *lens, const void *k_rows,
+                           const void *v_rows, int32_t n_tokens, int32_t first_kept, void *hip_stream);
+
+/*
+ * Rows read back as what they stand for, rounded to bf16: k_out, v_out [n_caches][n_rows][n_kv_heads][head_dim] receive rows
+ * first_rows[i] .. first_rows[i] + n_rows - 1 of cache i (first_rows NULL: from row 0).  VS_ERR_SHAPE if some of them are not
+ * among a cache's lens[i].  lens and first_rows are host memory.
+ */
+vs_status vs_cache8_read(const vs_shape *shape, int32_t n_caches, const void *slab, int32_t capacity, const int32_t *lens,
+                         const int32_t *first_rows, int32_t n_rows, void *k_out, void *v_out, void *hip_stream);
+
+/*
+ * vs_decode_attn over such caches: slab of n_streams caches; the step's rows k_new, v_new [n_streams][n_kv_heads][head_dim] (or
+ * both NULL) are quantised into row lens[s], lens[s] grows by one, and the query attends over all rows as what they stand
+ * for (the new one included).  Arguments, groups of 64 streams and errors otherwise as there; workspace:
+ * vs_cache8_workspace_bytes.
+ */
+vs_status vs_cache8_decode_attn(const vs_shape *shape, int32_t n_streams, void *slab, int32_t capacity, int32_t *lens, const void *q,
+                                const void *k_new, const void *v_new, void *out, void *workspace, size_t workspace_bytes,
+                                void *hip_stream);
+
+/*
+ * A frame's or a question's tokens over such a cache: token i sees the cache's len rows as what they stand for and
+ * rows 0 .. i of the run itself as they come, as in vs_frame_prefill_attn; then rows first_kept .. n_tokens - 1 of the run
+ * are quantised into the cache and len grows by their number (n_tokens - 1: the carrier; 0: all, as vs_question_prefill_append;
+ * n_tokens: none).  1 <= n_tokens <= 4096.  VS_ERR_CAPACITY, with nothing launched, if they do not fit; other errors
+ * as vs_frame_prefill_attn, but for VS_ERR_PLACEMENT: no part of this call relies on where workgroups run.  A value of the run that is
+ * not finite makes NaN of the outputs that it reaches, and of no others.
+ */
+vs_status vs_cache8_prefill_attn(const vs_shape *shape, vs_cache8 *cache, const void *q, const void *k_t, const void *v_t,
+                                 int32_t n_tokens, int32_t first_kept, void *out, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,7 +13,9 @@ EXPORTS = [
     "vs_carrier_compact_append", "vs_carrier_compact_append_batched", "vs_decode_attn",
     "vs_carrier_mean_pool", "vs_set_tuning", "vs_memory_bank_push", "vs_carrier_evict_append",
     "vs_frames_prefill_attn", "vs_decode_attn_static", "vs_question_prefill_append", "vs_frame_qkv_project",
-    "vs_rmsnorm", "vs_linear", "vs_frame_decoder_layer", "vs_linear_workspace_bytes", "vs_layer_workspace_bytes", "vs_memory_bank_workspace_bytes", "vs_frames_workspace_bytes",
+    "vs_rmsnorm", "vs_linear", "vs_frame_decoder_layer", "vs_rotary_plan_make", "vs_rotary", "vs_cache8_append", "vs_cache8_read",
+    "vs_cache8_decode_attn", "vs_cache8_prefill_attn",
+    "vs_cache8_bytes", "vs_cache8_workspace_bytes", "vs_linear_workspace_bytes", "vs_layer_workspace_bytes", "vs_memory_bank_workspace_bytes", "vs_frames_workspace_bytes",
     "vs_decode_static_scratch_bytes",
 ]
 
@@ -117,7 +119,17 @@ def lib():
         L.vs_frames_workspace_bytes.argtypes = [sp, i32, i32, i32]
         L.vs_frames_workspace_bytes.restype = sz
         L.vs_frame_qkv_project.argtypes = [sp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
-        for name in EXPORTS[2:-5]:
+        L.vs_rotary_plan_make.argtypes = [i32, ip, ctypes.c_double, i32, ctypes.POINTER(_CRotaryPlan)]
+        L.vs_rotary.argtypes = [sp, ctypes.POINTER(_CRotaryPlan), vp, i32, vp, vp, i32, vp, vp, vp]
+        L.vs_cache8_bytes.argtypes = [sp, i32]
+        L.vs_cache8_bytes.restype = sz
+        L.vs_cache8_workspace_bytes.argtypes = [sp, i32, i32, i32]
+        L.vs_cache8_workspace_bytes.restype = sz
+        L.vs_cache8_append.argtypes = [sp, i32, vp, i32, ip, vp, vp, i32, i32, vp]
+        L.vs_cache8_read.argtypes = [sp, i32, vp, i32, ip, ip, i32, vp, vp, vp]
+        L.vs_cache8_decode_attn.argtypes = [sp, i32, vp, i32, ip, vp, vp, vp, vp, vp, sz, vp]
+        L.vs_cache8_prefill_attn.argtypes = [sp, ctypes.POINTER(_CCache8), vp, vp, vp, i32, i32, vp, vp, sz, vp]
+        for name in EXPORTS[2:-7]:
             getattr(L, name).restype = ctypes.c_int
         _LIB = L
     return _LIB
@@ -368,6 +380,103 @@ def carrier_evict_append(shape, caches, first_row, bank_capacity, k_rows, v_rows
         if n and arr[0].len != caches[0].c.len:
             for c, a in zip(caches, arr):
                 c.c.len = a.len
+
+
+ROTARY_HALVES, ROTARY_ADJACENT = 0, 1
+
+
+class _CRotaryPlan(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("sections", ctypes.c_int32 * 3), ("pairing", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("turns", ctypes.c_double * 64)]
+
+
+class RotaryPlan:
+    """Which pairs of a head turn with which axis (time, height, width), and how fast: sections are pairs per axis."""
+
+    def __init__(self, head_dim, sections, theta=1e6, pairing=ROTARY_HALVES):
+        self.c = _CRotaryPlan()
+        _check(lib().vs_rotary_plan_make(head_dim, (ctypes.c_int32 * 3)(*sections), float(theta), int(pairing), ctypes.byref(self.c)),
+               "vs_rotary_plan_make")
+
+
+def rotary(shape, plan, positions, q, k, q_out, k_out, inverse=False, stream=None):
+    """positions: device int32 [3][T]; q, q_out [T][Hq][D], k, k_out [T][Hkv][D] (either pair may be None; in place: out is in)."""
+    _check(lib().vs_rotary(ctypes.byref(shape), ctypes.byref(plan.c), _ptr(positions), positions.shape[1], _ptr(q), _ptr(k), bool(inverse),
+                           _ptr(q_out), _ptr(k_out), _stream(stream)), "vs_rotary")
+
+
+class _CCache8(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("capacity", ctypes.c_int32), ("len", ctypes.c_int32)]
+
+
+def cache8_bytes(shape, capacity):
+    return int(lib().vs_cache8_bytes(ctypes.byref(shape), capacity))
+
+
+class Cache8:
+    """Retained K/V rows of one layer of one stream in 8 bits: a device uint8 tensor of cache8_bytes(shape, capacity) and a
+    host-side length, which may be lowered to any number of rows."""
+
+    def __init__(self, data, capacity, length=0):
+        assert data.is_contiguous() and data.element_size() == 1
+        self.data = data
+        self.c = _CCache8(data.data_ptr(), int(capacity), int(length))
+
+    @property
+    def len(self):
+        return self.c.len
+
+    @len.setter
+    def len(self, n):
+        self.c.len = int(n)
+
+    @property
+    def capacity(self):
+        return self.c.capacity
+
+
+def cache8_workspace_bytes(shape, max_q_tokens, max_cache_rows, n_streams):
+    return int(lib().vs_cache8_workspace_bytes(ctypes.byref(shape), max_q_tokens, max_cache_rows, n_streams))
+
+
+def make_cache8_workspace(shape, max_q_tokens, max_cache_rows, n_streams, device="cuda:0"):
+    """Allocate (torch uint8 tensor) and initialise a workspace for the calls over caches in 8 bits."""
+    import torch
+    n = cache8_workspace_bytes(shape, max_q_tokens, max_cache_rows, n_streams)
+    if n == 0:
+        raise VSError(3, "vs_cache8_workspace_bytes")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    workspace_init(shape, ws)
+    return ws
+
+
+def cache8_append(shape, slab, capacity, lens, k_rows, v_rows, first_kept=0, stream=None):
+    """slab: uint8 [n_caches][cache8_bytes]; lens: ctypes int32 array [n_caches] (host), grown by the rows kept;
+    k_rows, v_rows [n_caches][T][Hkv][D], rows first_kept.. of which are quantised into the caches."""
+    _check(lib().vs_cache8_append(ctypes.byref(shape), k_rows.shape[0], _ptr(slab), capacity, lens, _ptr(k_rows), _ptr(v_rows),
+                                  k_rows.shape[1], first_kept, _stream(stream)), "vs_cache8_append")
+
+
+def cache8_read(shape, slab, capacity, lens, first_rows, k_out, v_out, stream=None):
+    """Rows first_rows[i].. (None: 0..) of every cache as what they stand for -> k_out, v_out [n_caches][n][Hkv][D]."""
+    _check(lib().vs_cache8_read(ctypes.byref(shape), k_out.shape[0], _ptr(slab), capacity, lens, first_rows, k_out.shape[1],
+                                _ptr(k_out), _ptr(v_out), _stream(stream)), "vs_cache8_read")
+
+
+def cache8_decode_attn(shape, slab, capacity, lens, q, k_new, v_new, out, workspace, stream=None):
+    """decode_attn over a slab of caches in 8 bits; q, out [n_streams][Hq][D]."""
+    wp, wb = _ws(workspace)
+    _check(lib().vs_cache8_decode_attn(ctypes.byref(shape), q.shape[0], _ptr(slab), capacity, lens, _ptr(q), _ptr(k_new), _ptr(v_new),
+                                       _ptr(out), wp, wb, _stream(stream)), "vs_cache8_decode_attn")
+
+
+def cache8_prefill_attn(shape, cache, q, k_t, v_t, out, workspace, first_kept=None, stream=None):
+    """A run's tokens over a Cache8; rows first_kept.. of the run (None: the last, the carrier) are quantised into it."""
+    wp, wb = _ws(workspace)
+    n = q.shape[0]
+    _check(lib().vs_cache8_prefill_attn(ctypes.byref(shape), ctypes.byref(cache.c), _ptr(q), _ptr(k_t), _ptr(v_t), n,
+                                        n - 1 if first_kept is None else first_kept, _ptr(out), wp, wb, _stream(stream)),
+           "vs_cache8_prefill_attn")
 
 
 def carrier_mean_pool(e, c_out, dtype, stream=None):

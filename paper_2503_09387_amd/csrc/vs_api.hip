@@ -17,11 +17,6 @@ int g_tune_prefill_splits = 0;
 int g_tune_prefill_kv_groups = 0;
 int g_tune_decode_chunk_rows = 0;
 int g_tune_prefill_merge = 0;
-}  // namespace vs
-
-namespace {
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 vs_status check_shape(const vs_shape* s) {
     if (!s) return VS_ERR_NULL;
@@ -35,6 +30,11 @@ vs_status check_shape(const vs_shape* s) {
     if (s->dtype == VS_BF16 && s->head_dim != 128) return VS_ERR_UNSUPPORTED;
     return VS_OK;
 }
+}  // namespace vs
+
+namespace {
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 inline size_t elem_bytes(const vs_shape* s) { return s->dtype == VS_F32 ? 4 : 2; }
 inline int64_t row_bytes(const vs_shape* s) {

@@ -1,0 +1,83 @@
+// Retained rows in 8 bits: how a cache lies in memory, shared by the kernels that write it, read it back and attend over it.
+//
+// A row x of 128 values (one token, one KV head, K or V) is held as whole numbers q = rint(x / s), ties to even, beside
+// s = max(ceil8(max|x| / 127), 2^-126); ceil8 goes up to the next number of 8 significant bits, a bf16.  It stands for q * s.
+// x and s both have 8 significant bits, so a quotient that is no tie is further than 2^-17 of itself away from one,
+// and the quotient in fp32 rounds to the same whole number as the exact one: what is held does not depend on the arithmetic.
+// A row with a value that is not finite gets a scale that is not a number, and stands for nothing else.
+//
+// 32 rows of a KV head are a block of 8320 bytes: K codes, V codes, 32 scale pairs.  The codes lie as the matrix
+// instructions of the decode kernel take them, so that a wavefront moves a block from memory to the multiplier's registers with
+// ten loads of 16 bytes per lane and no exchange between lanes:
+//   K (A operand of 16 keys x 64 dims, lane = 16 h + key % 16, 16 bytes per lane): [key / 16][dims 64 ds ..][lane][16],
+//     bytes 0..7 of a lane: dims 64 ds + 8 h .., bytes 8..15: 64 ds + 32 + 8 h ..; two's complement
+//   V (A operand of 16 dims x 32 keys, lane = 16 h + dim / 8): [dim % 8][lane][8], two dims % 8 together in 16 bytes of a
+//     lane; bytes 4 kt + r of a lane: key 16 kt + 4 h + r, which is where the product of K leaves that key's score; code + 128
+//   scales: [key] (bf16 of K, bf16 of V)
+// Blocks are laid [block][KV head]; a cache is ceil(capacity / 32) * Hkv of them, and a cache of another capacity begins
+// with the same bytes.
+#pragma once
+#include "vs_internal.h"
+
+namespace vs {
+
+constexpr int kBlockRows = 32;
+constexpr int kBlockV = 4096, kBlockScales = 8192, kBlockBytes = 8320;  // offsets in a block, and its size: a multiple of 128
+
+inline int64_t cache8_bytes(const vs_shape& s, int32_t capacity) {
+    return ((int64_t)capacity + kBlockRows - 1) / kBlockRows * s.n_kv_heads * kBlockBytes;
+}
+
+// Where lane c of a row's 16 lanes (dims 8 c .. 8 c + 7) finds its 8 K codes of row `key` of a block.
+__device__ __forceinline__ int k_code_offset(int key, int c) {
+    return (((key >> 4) * 2 + (c >> 3)) * 64 + (c & 3) * 16 + (key & 15)) * 16 + ((c >> 2) & 1) * 8;
+}
+// And the V code of dim 8 c + dt of row `key`.
+__device__ __forceinline__ int v_code_offset(int key, int c, int dt) {
+    return kBlockV + (dt >> 1) * 1024 + (((key & 15) >> 2) * 16 + c) * 16 + (dt & 1) * 8 + (key >> 4) * 4 + (key & 3);
+}
+
+// The larger magnitudes of two pairs of bf16 bit patterns without their signs (K below, V above): as whole numbers they are
+// ordered as the values are, with infinities and then NaN above all.
+__device__ __forceinline__ unsigned max_pairs(unsigned a, unsigned b) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+// The scale's bf16 pattern for the largest magnitude's.
+__device__ __forceinline__ unsigned scale_bits(unsigned most) {
+    const unsigned up = (__float_as_uint(__uint_as_float(most << 16) / 127.0f) + 0xffffu) >> 16;
+    return most > 0x7f7fu ? 0x7fc0u : max(up, 0x80u);
+}
+// The largest magnitudes among 8 K and 8 V values (16 bytes each) of this lane and the row's 15 others.
+__device__ __forceinline__ unsigned row_most(const raw16& k, const raw16& v) {
+    unsigned a = max_pairs(max_pairs(k[0] & 0x7fff7fffu, k[1] & 0x7fff7fffu), max_pairs(k[2] & 0x7fff7fffu, k[3] & 0x7fff7fffu));
+    unsigned b = max_pairs(max_pairs(v[0] & 0x7fff7fffu, v[1] & 0x7fff7fffu), max_pairs(v[2] & 0x7fff7fffu, v[3] & 0x7fff7fffu));
+    unsigned m = max_pairs(__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(b, a, 0x07060302u));
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) m = max_pairs(m, __shfl_xor(m, o));
+    return m;
+}
+// The code of one of the two values in a word.
+__device__ __forceinline__ int code_of(unsigned pair, bool high, float scale) {
+    return (int)rintf(__uint_as_float(high ? pair & 0xffff0000u : pair << 16) / scale);
+}
+
+// K and V rows [n_caches][n_tokens][Hkv][128], their rows first_kept .. n_tokens - 1, quantised into the rows behind lens.v[i] of cache i
+// (at most kMaxStreamsPerLaunch caches).
+hipError_t launch_cache8_append(const vs_shape& s, int32_t n_caches, void* slab, int32_t capacity, const LenTable& lens, const void* k_rows,
+                                const void* v_rows, int32_t n_tokens, int32_t first_kept, hipStream_t st);
+// Rows first.v[i] .. first.v[i] + n_rows - 1 of cache i as what they stand for, rounded to bf16.
+hipError_t launch_cache8_read(const vs_shape& s, int32_t n_caches, const void* slab, int32_t capacity, const LenTable& first, int32_t n_rows,
+                              void* k_out, void* v_out, hipStream_t st);
+// lens: valid rows, the appended row included.
+size_t decode8_workspace_bytes(const vs_shape& s, int32_t n_streams);
+hipError_t launch_decode8(const vs_shape& s, int32_t n_streams, void* slab, int32_t capacity, const LenTable& lens, const void* q,
+                          const void* k_new, const void* v_new, void* out, void* workspace, hipStream_t st);
+// A run's n_tokens over the len rows of one cache and over one another.  Workspace: prefill8_workspace_need; prefill8_workspace_bytes for any run within
+// limits.
+size_t prefill8_workspace_need(const vs_shape& s, int32_t n_tokens, int32_t len);
+size_t prefill8_workspace_bytes(const vs_shape& s, int32_t max_tokens, int32_t max_len);
+hipError_t launch_prefill8(const vs_shape& s, const void* cache, int32_t len, const void* q, const void* k, const void* v, int32_t n_tokens,
+                           void* out, void* workspace, hipStream_t st);
+
+}  // namespace vs

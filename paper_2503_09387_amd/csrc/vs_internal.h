@@ -147,6 +147,9 @@ __device__ __forceinline__ unsigned count_in(unsigned* box, unsigned* word, int 
     return !seen ? 0u : last ? 2u : 1u;
 }
 
+// the rules that every shape is held to
+vs_status check_shape(const vs_shape* s);
+
 // the body of vs_decode_attn (checks, launches, length bookkeeping) over any workspace; stateless: nothing in
 // it has to hold anything when the call begins
 vs_status decode_entry(const vs_shape* shape, int32_t n_streams, void* k_slab, void* v_slab, int32_t capacity,
