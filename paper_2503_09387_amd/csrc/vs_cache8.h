@@ -57,9 +57,99 @@ __device__ __forceinline__ unsigned row_most(const raw16& k, const raw16& v) {
     for (int o = 1; o < 16; o <<= 1) m = max_pairs(m, __shfl_xor(m, o));
     return m;
 }
-// The code of one of the two values in a word.
-__device__ __forceinline__ int code_of(unsigned pair, bool high, float scale) {
-    return (int)rintf(__uint_as_float(high ? pair & 0xffff0000u : pair << 16) / scale);
+// Codes.  x / s to a rounding, or exactly where a product or a tie is: r = 1 / s to a rounding, then t = x r and what the remainder
+// x - t s adds.  (The division that the compiler writes takes twice the instructions.)  Below 2^-64 both go up by 2^64, where
+// the remainder has all its bits.
+struct Divisor {
+    float s, r, up;
+};
+__device__ __forceinline__ Divisor divisor_of(unsigned scale_bits) {
+    Divisor d;
+    d.s = __uint_as_float(scale_bits << 16);
+    d.up = d.s < 0x1p-64f ? 0x1p64f : 1.0f;
+    d.s *= d.up;
+    const float r = __builtin_amdgcn_rcpf(d.s);
+    d.r = fmaf(fmaf(-d.s, r, 1.0f), r, r);
+    return d;
+}
+// The code of one of the two values in a word, in the low byte (two's complement, plus 128 for V).
+template <bool kPlus128>
+__device__ __forceinline__ unsigned code_of(unsigned pair, bool high, const Divisor& d) {
+    const float x = __uint_as_float(high ? pair & 0xffff0000u : pair << 16) * d.up, t = x * d.r;
+    // (1.5 * 2^23 on top: the fraction goes, ties to even, and the whole number stands in the low bits)
+    return __float_as_uint(fmaf(fmaf(-t, d.s, x), d.r, t) + (kPlus128 ? 12583040.0f : 12582912.0f));
+}
+// The low bytes of four words as one.
+__device__ __forceinline__ unsigned bytes_of(unsigned a, unsigned b, unsigned c, unsigned d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+// The codes of a row's 16 bytes of K and of V in this lane, K's in two words, V's one a word, and the scale pair.
+__device__ __forceinline__ unsigned quantise(const raw16& k, const raw16& v, uint2& k_codes, unsigned (&v_codes)[8]) {
+    const unsigned most = row_most(k, v), ks = scale_bits(most & 0xffffu), vs = scale_bits(most >> 16);
+    const Divisor kd = divisor_of(ks), vd = divisor_of(vs);
+    unsigned w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        w[j] = code_of<false>(k[j >> 1], j & 1, kd);
+        v_codes[j] = code_of<true>(v[j >> 1], j & 1, vd);
+    }
+    k_codes = make_uint2(bytes_of(w[0], w[1], w[2], w[3]), bytes_of(w[4], w[5], w[6], w[7]));
+    return ks | (vs << 16);
+}
+
+// Rows at .. end - 1 of a cache, as far as they fall into the block at row0, from k, v (this lane's 16 bytes of row `at`, row_bytes apart), by a
+// wavefront: lane 16 h + c holds dims 8 c .. of the rows 16 kt + 4 h + r, so that rows are read whole, 256 bytes at a time, a row's
+// maximum is four exchanges among 16 lanes, and a lane ends up with all 8 keys that its V operand has side by side.
+__device__ __forceinline__ void write_block(char* blk, const char* k, const char* v, int64_t row_bytes, int row0, int at, int end, int lane) {
+    const int c = lane & 15, h = lane >> 4;
+    raw16 kx[8], vx[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int first = row0 + 16 * (u >> 2) + (u & 3);  // of four rows, 4 apart
+        if (first + 12 < at || first >= end) continue;
+        const int64_t off = (int64_t)(min(max(first + 4 * h, at), end - 1) - at) * row_bytes;  // (rows of others: not stored)
+        kx[u] = *reinterpret_cast<const raw16*>(k + off);
+        vx[u] = *reinterpret_cast<const raw16*>(v + off);
+    }
+    unsigned codes[8][8];
+    bool all = true;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int first = row0 + 16 * (u >> 2) + (u & 3), key = 16 * (u >> 2) + 4 * h + (u & 3), row = row0 + key;
+        if (first + 12 < at || first >= end) {
+            all = false;
+            continue;
+        }
+        const bool mine = row >= at && row < end;
+        all = all && mine;
+        uint2 k_codes;
+        const unsigned pair = quantise(kx[u], vx[u], k_codes, codes[u]);
+        if (mine) {
+            *reinterpret_cast<uint2*>(blk + k_code_offset(key, c)) = k_codes;
+            if (c == 0) *reinterpret_cast<unsigned*>(blk + kBlockScales + 4 * key) = pair;
+        }
+    }
+    if (all) {
+#pragma unroll
+        for (int dt = 0; dt < 8; dt += 2) {
+            raw16 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = dt + (i >> 1), u = 4 * (i & 1);
+                w[i] = bytes_of(codes[u][d], codes[u + 1][d], codes[u + 2][d], codes[u + 3][d]);
+            }
+            *reinterpret_cast<raw16*>(blk + kBlockV + (dt >> 1) * 1024 + lane * 16) = w;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int first = row0 + 16 * (u >> 2) + (u & 3), key = 16 * (u >> 2) + 4 * h + (u & 3), row = row0 + key;
+            if (first + 12 < at || first >= end) continue;
+            if (row >= at && row < end)
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) blk[v_code_offset(key, c, dt)] = (char)codes[u][dt];
+        }
+    }
 }
 
 // K and V rows [n_caches][n_tokens][Hkv][128], their rows first_kept .. n_tokens - 1, quantised into the rows behind lens.v[i] of cache i
@@ -77,7 +167,8 @@ hipError_t launch_decode8(const vs_shape& s, int32_t n_streams, void* slab, int3
 // limits.
 size_t prefill8_workspace_need(const vs_shape& s, int32_t n_tokens, int32_t len);
 size_t prefill8_workspace_bytes(const vs_shape& s, int32_t max_tokens, int32_t max_len);
-hipError_t launch_prefill8(const vs_shape& s, const void* cache, int32_t len, const void* q, const void* k, const void* v, int32_t n_tokens,
-                           void* out, void* workspace, hipStream_t st);
+// Rows first_kept .. of the run are quantised into the cache behind the len rows on the side.
+hipError_t launch_prefill8(const vs_shape& s, void* cache, int32_t len, const void* q, const void* k, const void* v, int32_t n_tokens,
+                           int32_t first_kept, void* out, void* workspace, hipStream_t st);
 
 }  // namespace vs

@@ -20,69 +20,17 @@ struct RowsParams {
     LenTable at;          // the cache's row that the first of them is
 };
 
-// A wavefront per (block, KV head): lane 16 h + c holds dims 8 c .. of the rows 16 kt + 4 h + r, so that rows are read whole, 256 bytes at a time,
-// a row's maximum is four exchanges among 16 lanes, and a lane ends up with all 8 keys that its V operand
-// has side by side.
+// A wavefront per (block, KV head).
 __global__ __launch_bounds__(kThreads) void cache8_append_kernel(RowsParams p) {
     const int lane = threadIdx.x & 63, item = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = lane & 15, h = lane >> 4;
-    const int len = p.at.v[blockIdx.y], block = len / kBlockRows + item / p.Hkv, g = item % p.Hkv;
-    const int row0 = block * kBlockRows, end = len + p.n_rows;
-    if (item >= p.items || row0 >= end) return;
-    char* const blk = p.slab + blockIdx.y * p.cache_bytes + ((int64_t)block * p.Hkv + g) * kBlockBytes;
-    const int64_t src = blockIdx.y * p.rows_stride + ((int64_t)g * 128 + 8 * c) * 2;
-    raw16 k[8], v[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        const int row = row0 + 16 * (u >> 2) + 4 * h + (u & 3);
-        const int64_t at = src + (int64_t)(min(max(row, len), end - 1) - len + p.first) * p.Hkv * 256;  // (rows of others: not stored)
-        k[u] = *reinterpret_cast<const raw16*>(p.k + at);
-        v[u] = *reinterpret_cast<const raw16*>(p.v + at);
-    }
-    unsigned codes[8][8];
-    bool all = true;
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        const int key = 16 * (u >> 2) + 4 * h + (u & 3), row = row0 + key;
-        const bool mine = row >= len && row < end;
-        all = all && mine;
-        const unsigned most = row_most(k[u], v[u]);
-        const unsigned ks = scale_bits(most & 0xffffu), vs = scale_bits(most >> 16);
-        const float kf = __uint_as_float(ks << 16), vf = __uint_as_float(vs << 16);
-        unsigned word[2] = {0u, 0u};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            word[j >> 2] |= (unsigned)(code_of(k[u][j >> 1], j & 1, kf) & 255) << (8 * (j & 3));
-            codes[j][u] = (unsigned)(code_of(v[u][j >> 1], j & 1, vf) + 128) & 255u;
-        }
-        if (mine) {
-            *reinterpret_cast<uint2*>(blk + k_code_offset(key, c)) = make_uint2(word[0], word[1]);
-            if (c == 0) *reinterpret_cast<unsigned*>(blk + kBlockScales + 4 * key) = ks | (vs << 16);
-        }
-    }
-    if (all) {
-#pragma unroll
-        for (int dt = 0; dt < 8; dt += 2) {
-            raw16 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const unsigned* x = &codes[dt + (i >> 1)][4 * (i & 1)];
-                w[i] = x[0] | (x[1] << 8) | (x[2] << 16) | (x[3] << 24);
-            }
-            *reinterpret_cast<raw16*>(blk + kBlockV + (dt >> 1) * 1024 + lane * 16) = w;
-        }
-    } else {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int key = 16 * (u >> 2) + 4 * h + (u & 3), row = row0 + key;
-            if (row >= len && row < end)
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt) blk[v_code_offset(key, c, dt)] = (char)codes[dt][u];
-        }
-    }
+    const int at = p.at.v[blockIdx.y], block = at / kBlockRows + item / p.Hkv, g = item % p.Hkv;
+    if (item >= p.items || block * kBlockRows >= at + p.n_rows) return;
+    const int64_t row_bytes = (int64_t)p.Hkv * 256, src = blockIdx.y * p.rows_stride + p.first * row_bytes + (int64_t)g * 256 + 16 * (lane & 15);
+    write_block(p.slab + blockIdx.y * p.cache_bytes + ((int64_t)block * p.Hkv + g) * kBlockBytes, p.k + src, p.v + src, row_bytes, block * kBlockRows, at,
+                at + p.n_rows, lane);
 }
 
-// The same lanes the other way round.
+// The lanes of write_block the other way round.
 __global__ __launch_bounds__(kThreads) void cache8_read_kernel(RowsParams p) {
     const int lane = threadIdx.x & 63, item = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, h = lane >> 4;
@@ -298,13 +246,8 @@ vs_status vs_cache8_prefill_attn(const vs_shape* shape, vs_cache8* cache, const 
     const size_t ctrl = control_block_bytes(*shape);
     if (!workspace || workspace_bytes < ctrl + prefill8_workspace_need(*shape, n_tokens, len)) return VS_ERR_WORKSPACE;
     if (!aligned16(workspace)) return VS_ERR_ALIGN;
-    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (launch_prefill8(*shape, cache->data, len, q, k_t, v_t, n_tokens, out, static_cast<char*>(workspace) + ctrl, stream) != hipSuccess)
-        return VS_ERR_HIP;
-    LenTable t{};
-    t.v[0] = len;
-    if (n_kept > 0 &&
-        launch_cache8_append(*shape, 1, cache->data, cache->capacity, t, k_t, v_t, n_tokens, first_kept, stream) != hipSuccess)
+    if (launch_prefill8(*shape, cache->data, len, q, k_t, v_t, n_tokens, first_kept, out, static_cast<char*>(workspace) + ctrl,
+                        static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return VS_ERR_HIP;
     cache->len += n_kept;
     return VS_OK;

@@ -197,18 +197,15 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(Decode8Params p) {
         const int key = (len - 1) % kBlockRows;
         const int64_t at = ((int64_t)s * p.Hkv + g) * 256 + 16 * i16;
         const raw16 k = *reinterpret_cast<const raw16*>(p.k_new + at), v = *reinterpret_cast<const raw16*>(p.v_new + at);
-        const unsigned most = row_most(k, v), ks = scale_bits(most & 0xffffu), vs = scale_bits(most >> 16);
         char* const blk = base + (n_blocks - 1) * stride;
+        uint2 k_codes;
+        unsigned v_codes[8];
+        const unsigned pair = quantise(k, v, k_codes, v_codes);
         if (h == 0) {
-            const float kf = __uint_as_float(ks << 16), vf = __uint_as_float(vs << 16);
-            unsigned word[2] = {0u, 0u};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                word[j >> 2] |= (unsigned)(code_of(k[j >> 1], j & 1, kf) & 255) << (8 * (j & 3));
-                blk[v_code_offset(key, i16, j)] = (char)(code_of(v[j >> 1], j & 1, vf) + 128);
-            }
-            *reinterpret_cast<uint2*>(blk + k_code_offset(key, i16)) = make_uint2(word[0], word[1]);
-            if (i16 == 0) *reinterpret_cast<unsigned*>(blk + kBlockScales + 4 * key) = ks | (vs << 16);
+            for (int j = 0; j < 8; ++j) blk[v_code_offset(key, i16, j)] = (char)v_codes[j];
+            *reinterpret_cast<uint2*>(blk + k_code_offset(key, i16)) = k_codes;
+            if (i16 == 0) *reinterpret_cast<unsigned*>(blk + kBlockScales + 4 * key) = pair;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");  // the wavefront reads what its lanes have just written
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

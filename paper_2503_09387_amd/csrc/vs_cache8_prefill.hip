@@ -10,9 +10,12 @@
 //   * p s_v in bf16 (8 bits, as P does over caches in bf16; the denominator sums p before that) times the codes + 128 in bf16, which
 //     loses nothing, less 128 times the sum of p s_v, through one more product.
 // The G query heads of a KV head are packed into rows (row = token * G + head).  A wavefront holds 32 rows (two sets of 16 columns) and walks
-// blocks of 32 keys, which come from memory in the multiplier's own order (vs_cache8.h): nothing is staged, no barrier is met before the
-// end.  A workgroup is 8 wavefronts, kRT row tiles x 8 / kRT key groups: the row tiles of a group load the same blocks at about the same
-// time (the compute unit's cache serves all but the first), the key groups are added in LDS.
+// blocks of 32 keys.  A workgroup is 8 wavefronts, kRT row tiles x 8 / kRT key groups, which are added in LDS at the end:
+//   * kRT = 4: two key groups, a wavefront of each on every SIMD.  A block comes from memory once, a quarter by each wavefront of
+//     its group, which widens its quarter into LDS for all four (widening costs as many vector instructions as the softmax of 32 rows).
+//     The groups take turns, a barrier apart: while one multiplies (the last block's values, the next one's keys), the other works out
+//     probabilities and widens, so that matrix and vector instructions of a SIMD run side by side.
+//   * kRT = 1, for up to 64 rows: every wavefront has a block of its own, straight from memory into the multiplier.
 #include "vs_cache8.h"
 
 #include <algorithm>
@@ -22,7 +25,6 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
@@ -32,9 +34,10 @@ constexpr int kTileRows = 32;  // rows of a wavefront
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazyMax = 8.0f;  // scores may exceed the reference maximum by 2^8 before it is refreshed
 constexpr int kMaxSplits = 32;
+constexpr int kAhead = 5;       // pieces of a block that are on their way from LDS
 
 struct Prefill8Params {
-    const char* cache;
+    char* cache;
     const char* q;
     const char* k;   // the run's own rows
     const char* v;
@@ -45,66 +48,188 @@ struct Prefill8Params {
     int n_cache_blocks;
     int n_groups;      // row groups: kRT * 32 rows each
     int nsplit;
+    int first_kept;    // rows of the run from this one on are kept,
+    int n_keeping;     // (block, KV head) pairs that they fall into
+    unsigned by_G;     // row / G: the upper half of row * by_G (G > 1)
     float scale_log2e;
 };
 
-// A block of cached rows in a wavefront's registers.
-struct Block {
-    raw16 k[4], v[4], s[2];
-};
-__device__ __forceinline__ void fetch_keys(Block& b, const char* blk, int lane) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) b.k[j] = *reinterpret_cast<const raw16*>(blk + j * 1024 + lane * 16);
-}
-__device__ __forceinline__ void fetch_scales(Block& b, const char* blk, int lane) {
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) b.s[kt] = *reinterpret_cast<const raw16*>(blk + kBlockScales + 64 * kt + 16 * (lane >> 4));
-}
-__device__ __forceinline__ void fetch_values(Block& b, const char* blk, int lane) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) b.v[j] = *reinterpret_cast<const raw16*>(blk + kBlockV + j * 1024 + lane * 16);
-}
-
 struct State {
-    f32x4 o[2][8];    // [columns][dim % 8]: element r of lane (column i16, h): dim 8 (4 h + r) + dim % 8
-    f32x4 excess[2];  // 128 times the sum of p s_v, negative
-    float m[2], l[2]; // reference (log2 units), this lane's share of the sum
+    f32x4 o[2][8];     // [columns][dim % 8]: element r of lane (column i16, h): dim 8 (4 h + r) + dim % 8
+    f32x4 excess[2];   // 128 times the sum of p s_v, negative
+    float m[2], l[2];  // reference (log2 units; 0 until a key has been seen), this lane's share of the sum
+    float limit[2];    // how far scores may pass the reference before it is refreshed: -INFINITY until a key has been seen
 };
 
-// The softmax of a block's scores z f (f: the same for a column's lanes) and the product with V.  Codes: 8 words of V (4 words of 4 codes + 128 for two dims % 8
-// each); else 32 words of bf16 pairs.
-template <typename VOf>
-__device__ __forceinline__ void accumulate(State& st, float (&z)[2][8], const float (&f)[2], const float* sv, VOf v_of) {
-    float mx[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-        mx[c] = f[c] * fmaxf(fmaxf(fmaxf(z[c][0], z[c][1]), fmaxf(z[c][2], z[c][3])), fmaxf(fmaxf(z[c][4], z[c][5]), fmaxf(z[c][6], z[c][7])));
-    if (__any(mx[0] > st.m[0] + kLazyMax || mx[1] > st.m[1] + kLazyMax)) {  // rare after the first block
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            float x = fmaxf(mx[c], __shfl_xor(mx[c], 16));
-            x = fmaxf(x, __shfl_xor(x, 32));
-            // (-INFINITY: a row that sees none of these keys and has seen none before)
-            const float m_new = fmaxf(st.m[c], x), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[c] - m_new);
-            st.m[c] = m_new;
-            st.l[c] *= alpha;
-            st.excess[c] *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) st.o[c][dt] *= alpha;
-        }
-    }
-    bf16x8 p[2];
+// (fmaxf of values that come out of a selection is three instructions for one)
+__device__ __forceinline__ float max_of_8(const float (&z)[8]) {
+    float a, b;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(z[0]), "v"(z[1]), "v"(z[2]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(z[3]), "v"(z[4]), "v"(z[5]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(z[6]), "v"(z[7]), "v"(a));
+    asm("v_max_f32 %0, %1, %2" : "=v"(a) : "v"(a), "v"(b));
+    return a;
+}
+
+// four codes of V as bf16: whole numbers 0..255, whose fp32 has nothing in its lower half
+__device__ __forceinline__ void widen(unsigned w, unsigned& lo, unsigned& hi) {
+    const unsigned a = __float_as_uint((float)(w & 255u)), b = __float_as_uint((float)((w >> 8) & 255u));
+    const unsigned c = __float_as_uint((float)((w >> 16) & 255u)), d = __float_as_uint((float)(w >> 24));
+    lo = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    hi = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+
+// The queries of a wavefront's columns as fp16, what the sums over codes + 1152 start at, and the factor of the scores.
+struct Queries {
+    f16x8 q[2][4];
+    float start[2], f[2];
+};
+__device__ __forceinline__ void take_queries(Queries& out, const raw16 (&w)[2][4], float scale_log2e) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-        const float m = st.m[c] == -INFINITY ? 0.f : st.m[c];
+        unsigned most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float pe = __builtin_amdgcn_exp2f(fmaf(z[c][e], f[c], -m));
-            st.l[c] += pe;
-            p[c][e] = (__bf16)(sv ? pe * sv[e] : pe);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) most = max_pairs(most, w[c][i][j] & 0x7fff7fffu);
+        most = max(most & 0xffffu, most >> 16);
+        most = max(most, (unsigned)__shfl_xor((int)most, 16));
+        most = max(most, (unsigned)__shfl_xor((int)most, 32));
+        // (up to 2^126: the smallest bf16 is then 2^-7, an fp16 like any other)
+        const int up = min(14 + 127 - (int)(most >> 7), 126);
+        const float factor = __uint_as_float((unsigned)(127 + up) << 23);
+        const unsigned minus1152 = 0xe480e480u;
+        const f16x8 off = __builtin_bit_cast(f16x8, u32x4{minus1152, minus1152, minus1152, minus1152});
+        f32x4 start = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned pair = w[c][i][j >> 1];
+                out.q[c][i][j] = (_Float16)(__uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16) * factor);
+            }
+            start = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, out.q[c][i], start, 0, 0, 0);
+        }
+        out.start[c] = start[0];
+        // (a query that is not finite gives scores that are not numbers; a factor of 0 would make them of what is masked)
+        out.f[c] = most > 0x7f7fu ? __uint_as_float(0x7fc00000u) : fmaxf(ldexpf(scale_log2e, -up), 1.17549435e-38f);
+    }
+}
+
+// four codes of K as fp16, 1152 too large
+__device__ __forceinline__ void widen_key(unsigned w, unsigned& lo, unsigned& hi) {
+    w ^= 0x80808080u;
+    lo = __builtin_amdgcn_perm(0x64646464u, w, 0x05010400u);
+    hi = __builtin_amdgcn_perm(0x64646464u, w, 0x07030602u);
+}
+__device__ __forceinline__ f16x8 keys_of(unsigned x, unsigned y) {
+    u32x4 a;
+    unsigned lo, hi;
+    widen_key(x, lo, hi);
+    a[0] = lo, a[1] = hi;
+    widen_key(y, lo, hi);
+    a[2] = lo, a[3] = hi;
+    return __builtin_bit_cast(f16x8, a);
+}
+// 8 V codes + 128 as bf16
+__device__ __forceinline__ bf16x8 values_of(unsigned x, unsigned y) {
+    u32x4 a;
+    unsigned lo, hi;
+    widen(x, lo, hi);
+    a[0] = lo, a[1] = hi;
+    widen(y, lo, hi);
+    a[2] = lo, a[3] = hi;
+    return __builtin_bit_cast(bf16x8, a);
+}
+
+// x *= f in the registers where x is: written as products, the compiler gives the sums other registers behind the branch around
+// them, and copies them on every turn.
+__device__ __forceinline__ void scale_in_place(f32x4& x, float f) {
+    float a = x[0], b = x[1], c = x[2], d = x[3];
+    asm volatile("v_mul_f32 %0, %0, %4\n\tv_mul_f32 %1, %1, %4\n\tv_mul_f32 %2, %2, %4\n\tv_mul_f32 %3, %3, %4" : "+v"(a), "+v"(b), "+v"(c), "+v"(d) : "v"(f));
+    x = f32x4{a, b, c, d};
+}
+
+// Scores less the reference become probabilities; the sums take them.
+__device__ __forceinline__ void soften(State& st, float (&x)[2][8]) {
+    const float mx[2] = {max_of_8(x[0]), max_of_8(x[1])};
+    if (__any(mx[0] > st.limit[0] || mx[1] > st.limit[1])) {  // rare after the first block
+        asm volatile("s_nop 15\n\ts_nop 15");  // (the last matrix instruction's sums, before assembly that the compiler does not look into)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const bool seen = st.limit[c] != -INFINITY;
+            float up = fmaxf(mx[c], __shfl_xor(mx[c], 16));
+            up = fmaxf(up, __shfl_xor(up, 32));
+            if (seen) up = fmaxf(up, 0.f);
+            if (up == -INFINITY) up = 0.f;  // (the column sees none of these keys and has seen none before)
+            else st.limit[c] = kLazyMax;
+            const float keep = seen ? __builtin_amdgcn_exp2f(-up) : 1.f;
+            st.m[c] += up;
+            st.l[c] *= keep;
+            scale_in_place(st.excess[c], keep);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) scale_in_place(st.o[c][dt], keep);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[c][e] -= up;
         }
     }
-    if (sv) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[c][e] = __builtin_amdgcn_exp2f(x[c][e]);
+            st.l[c] += x[c][e];
+        }
+}
+
+// The three steps of a block of cached rows.  Scores of its keys (k_of(kt, i): 16 keys, 32 dims):
+template <typename KOf>
+__device__ __forceinline__ void multiply_keys(f32x4 (&s)[2][2], const Queries& q, KOf k_of) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) s[kt][c] = f32x4{q.start[c], q.start[c], q.start[c], q.start[c]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const f16x8 k = k_of(kt, i);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) s[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q.q[c][i], s[kt][c], 0, 0, 0);
+        }
+}
+// probabilities times the scales of V, of the first `valid` rows:
+template <typename Then>
+__device__ __forceinline__ void weigh(State& st, bf16x8 (&p)[2], const f32x4 (&s)[2][2], const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Queries& q,
+                                      int valid, int h, Then then) {
+    float x[2][8], v[8];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) x[c][4 * kt + r] = fmaf(s[kt][c][r], ks[kt][r] * q.f[c], -st.m[c]);
+            v[4 * kt + r] = vs[kt][r];
+        }
+    if (valid < kBlockRows) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (16 * (e >> 2) + 4 * h + (e & 3) >= valid) {
+                x[0][e] = x[1][e] = -INFINITY;
+                v[e] = 0.f;
+            }
+    }
+    soften(st, x);
+    then();
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)(x[c][e] * v[e]);
+}
+// and their product with the values (v_of(dt): dims % 8 = dt of 32 keys).
+template <bool kCodes, typename VOf>
+__device__ __forceinline__ void multiply_values(State& st, const bf16x8 (&p)[2], VOf v_of) {
+    if (kCodes) {
         const unsigned minus128 = 0xc300c300u;
         const bf16x8 off = __builtin_bit_cast(bf16x8, u32x4{minus128, minus128, minus128, minus128});
 #pragma unroll
@@ -118,90 +243,39 @@ __device__ __forceinline__ void accumulate(State& st, float (&z)[2][8], const fl
     }
 }
 
-// four codes of V as bf16: whole numbers 0..255, whose fp32 has nothing in its lower half
-__device__ __forceinline__ void widen(unsigned w, unsigned& lo, unsigned& hi) {
-    const unsigned a = __float_as_uint((float)(w & 255u)), b = __float_as_uint((float)((w >> 8) & 255u));
-    const unsigned c = __float_as_uint((float)((w >> 16) & 255u)), d = __float_as_uint((float)(w >> 24));
-    lo = __builtin_amdgcn_perm(b, a, 0x07060302u);
-    hi = __builtin_amdgcn_perm(d, c, 0x07060302u);
-}
-
-// One block of cached rows, of which `valid` are there; the next block is asked for piece by piece as this one's are used up.
-__device__ __forceinline__ void attend_cached(State& st, Block& b, const char* next, const f16x8 (&q)[2][4], const float (&start)[2], const float (&f)[2],
-                                              int valid, int lane) {
-    const int h = lane >> 4;
-    float z[2][8], sv[8];
-    f32x4 s[2][2];
+// The keys of a block of the run's own rows, keys 32 j .., as the products take them.
+__device__ __forceinline__ void ask_own_keys(bf16x8 (&to)[2][4], const char* k, int64_t row_bytes, int j, int T, int i16, int h) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) s[kt][c] = f32x4{start[c], start[c], start[c], start[c]};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned x = b.k[2 * kt + (i >> 1)][2 * (i & 1)] ^ 0x80808080u, y = b.k[2 * kt + (i >> 1)][2 * (i & 1) + 1] ^ 0x80808080u;
-            const f16x8 k = __builtin_bit_cast(f16x8, u32x4{__builtin_amdgcn_perm(0x64646464u, x, 0x05010400u), __builtin_amdgcn_perm(0x64646464u, x, 0x07030602u),
-                                                            __builtin_amdgcn_perm(0x64646464u, y, 0x05010400u), __builtin_amdgcn_perm(0x64646464u, y, 0x07030602u)});
-#pragma unroll
-            for (int c = 0; c < 2; ++c) s[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[c][i], s[kt][c], 0, 0, 0);
-        }
-    }
-    fetch_keys(b, next, lane);
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const unsigned pair = b.s[kt][r];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) z[c][4 * kt + r] = s[kt][c][r] * __uint_as_float(pair << 16);
-            sv[4 * kt + r] = __uint_as_float(pair & 0xffff0000u);
-        }
-    fetch_scales(b, next, lane);
-    if (valid < kBlockRows) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (16 * (e >> 2) + 4 * h + (e & 3) >= valid) {
-                z[0][e] = z[1][e] = -INFINITY;
-                sv[e] = 0.f;
-            }
-    }
-    accumulate(st, z, f, sv, [&](int dt) {
-        u32x4 a;
-        unsigned x, y;
-        widen(b.v[dt >> 1][2 * (dt & 1)], x, y);
-        a[0] = x, a[1] = y;
-        widen(b.v[dt >> 1][2 * (dt & 1) + 1], x, y);
-        a[2] = x, a[3] = y;
-        return __builtin_bit_cast(bf16x8, a);
-    });
-    fetch_values(b, next, lane);
-}
-
-// One block of the run's own rows, keys 32 j ..: column c sees keys up to `last[c]` of them.
-__device__ __forceinline__ void attend_own(State& st, const char* k, const char* v, int64_t row_bytes, int j, int T, const bf16x8 (&q)[2][4],
-                                           const float (&f)[2], const int (&last)[2], int i16, int h) {
-    float z[2][8];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-        f32x4 s[2];
-        s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
         const char* const row = k + min(32 * j + 16 * kt + i16, T - 1) * row_bytes + 16 * h;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bf16x8 a = *reinterpret_cast<const bf16x8*>(row + 64 * i);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) s[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[c][i], s[c], 0, 0, 0);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) z[c][4 * kt + r] = 32 * j + 16 * kt + 4 * h + r <= last[c] ? s[c][r] : -INFINITY;
+        for (int i = 0; i < 4; ++i) to[kt][i] = *reinterpret_cast<const bf16x8*>(row + 64 * i);
     }
+}
+// Such a block: column c sees keys up to `last[c]` of the run.  The keys of block j + step are asked for on the way.
+__device__ __forceinline__ void attend_own(State& st, bf16x8 (&keys)[2][4], const char* k, const char* v, int64_t row_bytes, int j, int step, int T,
+                                           const raw16 (&q)[2][4], float f, const int (&last)[2], int i16, int h) {
     raw16 x[8];  // 8 keys, of each dims 8 i16 ..
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int key = 32 * j + 16 * (e >> 2) + 4 * h + (e & 3);
         x[e] = *reinterpret_cast<const raw16*>(v + min(key, T - 1) * row_bytes + 16 * i16);
     }
+    float z[2][8];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+        f32x4 s[2];
+        s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) s[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys[kt][i], __builtin_bit_cast(bf16x8, q[c][i]), s[c], 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) z[c][4 * kt + r] = 32 * j + 16 * kt + 4 * h + r <= last[c] ? fmaf(s[c][r], f, -st.m[c]) : -INFINITY;
+    }
+    ask_own_keys(keys, k, row_bytes, j + step, T, i16, h);
     auto columns_of = [](const raw16 (&w)[8], int dt) {  // the 8 keys' values of dim % 8 = dt
         u32x4 a;
 #pragma unroll
@@ -216,49 +290,80 @@ __device__ __forceinline__ void attend_own(State& st, const char* k, const char*
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = max_pairs(most, x[e][i] & 0x7fff7fffu);
     if (__any(max(most & 0xffffu, most >> 16) > 0x7f7fu)) {
-        raw16 odd[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const unsigned lo = (x[e][i] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (x[e][i] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-                odd[e][i] = (lo | hi) & 0x3f803f80u;  // 1 for each
-                x[e][i] &= ~(lo | hi);
-            }
         bf16x8 sees[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int e = 0; e < 8; ++e) sees[c][e] = (__bf16)(32 * j + 16 * (e >> 2) + 4 * h + (e & 3) <= last[c] ? 1.f : 0.f);
+        auto bad = [](unsigned w) {  // ones where a half is not finite
+            const unsigned top = ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+            return top | (top - (top >> 15));
+        };
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt)
+        for (int dt = 0; dt < 8; ++dt) {
+            u32x4 odd;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned a = x[2 * i][dt >> 1], b = x[2 * i + 1][dt >> 1];
+                odd[i] = bad(dt & 1 ? (a >> 16) | (b & 0xffff0000u) : (a & 0xffffu) | (b << 16)) & 0x3f803f80u;
+            }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(columns_of(odd, dt), sees[c], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), sees[c], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     if (n[r] > 0.f) st.o[c][dt][r] = __uint_as_float(0x7fc00000u);
             }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[e][i] &= ~bad(x[e][i]);
     }
-    accumulate(st, z, f, nullptr, [&](int dt) { return columns_of(x, dt); });
+    soften(st, z);
+    bf16x8 p[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)z[c][e];
+    multiply_values<false>(st, p, [&](int dt) { return columns_of(x, dt); });
 }
 
-// Grid: (splits * row groups * Hkv, as workgroups that share the keys of a row group lie side by side).
+// Grid (splits, Hkv, row groups and more): workgroups that read the same keys are Hkv * splits apart.  Those beyond the row groups quantise the
+// rows that are kept, a block and KV head each wavefront; whoever attends to the block they go to leaves out rows from len on.
 template <int kRT>
 __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p) {
     constexpr int kKG = kWaves / kRT;
-    constexpr int kRowStride = D + 4;
-    __shared__ __attribute__((aligned(16))) float s_o[kWaves / 2][kTileRows][kRowStride];
-    __shared__ float s_m[kWaves / 2][kTileRows], s_l[kWaves / 2][kTileRows];
+    constexpr bool kShared = kRT > 1;
+    static_assert(!kShared || kKG == 2, "two key groups take turns");
+    constexpr int kStaged = 16384 + 256;  // a widened block: K, V, the scales of K, the scales of V
+    constexpr int kLds = 16 * (8 * 64 * 4 + 32) * 4;  // both sets of columns of 8 wavefronts
+    __shared__ __attribute__((aligned(16))) char smem[kLds];
+    static_assert(3 * 2 * kStaged <= kLds, "three blocks of either key group: one each that values, keys and widening are at");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i16 = lane & 15, h = lane >> 4;
-    const int split = blockIdx.x % p.nsplit, unit = blockIdx.x / p.nsplit, g = unit % p.Hkv, group = unit / p.Hkv;
+    const int split = blockIdx.x, g = blockIdx.y, group = blockIdx.z;
+    auto token_of = [&](int row) { return p.G == 1 ? row : (int)__umulhi((unsigned)row, p.by_G); };
+    if (group >= p.n_groups) {
+        const int item = (((group - p.n_groups) * p.Hkv + g) * p.nsplit + split) * kWaves + wave;
+        if (item >= p.n_keeping) return;
+        const int kept = p.T - p.first_kept, block = p.len / kBlockRows + item / p.Hkv, head = item % p.Hkv;
+        const int64_t row_bytes = (int64_t)p.Hkv * 256, src = p.first_kept * row_bytes + head * 256 + 16 * i16;
+        write_block(p.cache + ((int64_t)block * p.Hkv + head) * kBlockBytes, p.k + src, p.v + src, row_bytes, block * kBlockRows, p.len, p.len + kept, lane);
+        return;
+    }
     const int rt = wave % kRT, kg = wave / kRT;
     const int row0 = (group * kRT + rt) * kTileRows;
     // blocks that rows of the group see: the cache's and the run's own up to its last token
     const int last_row = min((group + 1) * kRT * kTileRows, p.M) - 1;
-    const int n_blocks = p.n_cache_blocks + last_row / p.G / 32 + 1;
-    const int first = (int)((int64_t)n_blocks * split / p.nsplit), end = (int)((int64_t)n_blocks * (split + 1) / p.nsplit);
+    // (an own block takes about twice a cached one's time: the shares are even in that measure)
+    const unsigned total = p.n_cache_blocks + 2 * (token_of(last_row) / 32 + 1), share = total / p.nsplit, more = total - share * p.nsplit;
+    auto border = [&](int s) {
+        const int at = s * share + min((unsigned)s, more);
+        return at <= p.n_cache_blocks ? at : p.n_cache_blocks + (at - p.n_cache_blocks + 1) / 2;
+    };
+    const int first = border(split), end = border(split + 1);
+    const int stop = min(end, p.n_cache_blocks);
     const char* const base = p.cache + (int64_t)g * kBlockBytes;
     const int64_t stride = (int64_t)p.Hkv * kBlockBytes, row_bytes = (int64_t)p.Hkv * 256;
 
@@ -268,160 +373,270 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) st.o[c][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         st.excess[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-        st.m[c] = -INFINITY;
-        st.l[c] = 0.f;
+        st.m[c] = st.l[c] = 0.f;
+        st.limit[c] = -INFINITY;
     }
-    if (row0 < p.M) {
-        int b = first + kg;
-        const char* q_row[2];
-        int last[2];
+    raw16 query[2][4];
+    int last[2];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const int row = min(row0 + 16 * c + i16, p.M - 1), t = row / p.G;
-            q_row[c] = p.q + (((int64_t)t * p.Hq + (int64_t)g * p.G + row - t * p.G) * D + 8 * h) * 2;
-            last[c] = t;
+    for (int c = 0; c < 2; ++c) {
+        const int row = min(row0 + 16 * c + i16, p.M - 1), t = token_of(row);
+        const char* const at = p.q + (((int64_t)t * p.Hq + (int64_t)g * p.G + row - t * p.G) * D + 8 * h) * 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) query[c][i] = *reinterpret_cast<const raw16*>(at + 64 * i);
+        last[c] = t;
+    }
+    // the run's own blocks
+    auto own_blocks = [&] {
+        int j = max(first, p.n_cache_blocks) + kg - p.n_cache_blocks;
+        const int own_end = end - p.n_cache_blocks;
+        if (j >= own_end) return;
+        const char *const k = p.k + (int64_t)g * 256, *const v = p.v + (int64_t)g * 256;
+        bf16x8 keys[2][4];
+        ask_own_keys(keys, k, row_bytes, j, p.T, i16, h);
+        for (; j < own_end; j += kKG) attend_own(st, keys, k, v, row_bytes, j, kKG, p.T, query, p.scale_log2e, last, i16, h);
+    };
+    int b = first + kg;  // the block that this wavefront is at
+    if constexpr (kShared) {
+        raw16 k{}, v{}, k1{}, v1{};
+        unsigned pair = 0, pair1 = 0;
+        auto ask = [&](int block) {  // a quarter of a block (behind the last one: that one again)
+            const char* const blk = base + min(block, stop - 1) * stride;
+            k = *reinterpret_cast<const raw16*>(blk + rt * 1024 + lane * 16);
+            v = *reinterpret_cast<const raw16*>(blk + kBlockV + rt * 1024 + lane * 16);
+            pair = *reinterpret_cast<const unsigned*>(blk + kBlockScales + 4 * (lane & 31));
+        };
+        auto widen_into = [&](int buffer) {
+            char* const to = smem + (2 * buffer + kg) * kStaged;
+            char* const mine = to + rt * 2048 + lane * 16;
+            *reinterpret_cast<f16x8*>(mine) = keys_of(k[0], k[1]);
+            *reinterpret_cast<f16x8*>(mine + 1024) = keys_of(k[2], k[3]);
+            *reinterpret_cast<bf16x8*>(mine + 8192) = values_of(v[0], v[1]);
+            *reinterpret_cast<bf16x8*>(mine + 9216) = values_of(v[2], v[3]);
+            // (by all four, the same)
+            *reinterpret_cast<float*>(to + 16384 + 4 * lane) = __uint_as_float(lane < 32 ? pair << 16 : pair & 0xffff0000u);
+        };
+        if (first < stop) {
+            ask(b + 2);
+            k1 = k, v1 = v, pair1 = pair;
+            ask(b);
         }
-        if (b < end && b < p.n_cache_blocks) {
-            Block x;
-            const int stop = min(end, p.n_cache_blocks);
-            const char* blk = base + b * stride;
-            fetch_keys(x, blk, lane);
-            fetch_scales(x, blk, lane);
-            fetch_values(x, blk, lane);
-            f16x8 q[2][4];
-            float start[2], f[2];
+        own_blocks();  // (first: their queries are there as they are needed, and the cache's first blocks come meanwhile)
+        if (first < stop) {
+            Queries q;
+            take_queries(q, query, p.scale_log2e);
+            widen_into(0);
+            k = k1, v = v1, pair = pair1;
+            __syncthreads();
+            if (kg == 1) __syncthreads();  // half a turn behind the other group
+            const int turns = (stop - first + 1) / 2;
+            f32x4 s[2][2];
+            bf16x8 weights[2];
+            int next = 1;
+            const char* block = smem + kg * kStaged;
+            multiply_keys(s, q, [&](int kt, int i) { return *reinterpret_cast<const f16x8*>(block + (4 * kt + i) * 1024 + lane * 16); });
+            widen_into(next);
+            ask(b + 4);
+            for (int turn = 0; turn < turns; ++turn, b += 2) {
+                __syncthreads();
+                f32x4 ks[2], vs[2];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                raw16 w[4];
-                unsigned most = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[i] = *reinterpret_cast<const raw16*>(q_row[c] + 64 * i);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) most = max_pairs(most, w[i][j] & 0x7fff7fffu);
+                for (int kt = 0; kt < 2; ++kt) {
+                    ks[kt] = *reinterpret_cast<const f32x4*>(block + 16384 + 64 * kt + 16 * h);
+                    vs[kt] = *reinterpret_cast<const f32x4*>(block + 16384 + 128 + 64 * kt + 16 * h);
                 }
-                most = max(most & 0xffffu, most >> 16);
-                most = max(most, (unsigned)__shfl_xor((int)most, 16));
-                most = max(most, (unsigned)__shfl_xor((int)most, 32));
-                const int up = 14 + 127 - max((int)(most >> 7), 1);
-                float sum = 0.f;
+                raw16 piece[16];  // of V, then of the next block's K
+                const char* const after = smem + (2 * next + kg) * kStaged;
+                auto take = [&](int i) {
+                    piece[i] = *reinterpret_cast<const raw16*>(i < 8 ? block + 8192 + i * 1024 + lane * 16 : after + (i - 8) * 1024 + lane * 16);
+                };
+                weigh(st, weights, s, ks, vs, q, b < stop ? p.len - b * kBlockRows : 0, h, [&] {  // (no block is left: none of its rows count)
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < kAhead; ++i) take(i);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                __syncthreads();
+                // The products, in this order: pieces come from LDS kAhead steps before they are multiplied, and a word is widened at a step.
+                __builtin_amdgcn_s_setprio(1);
+                next = next == 2 ? 0 : next + 1;
+                char* const to = smem + (2 * next + kg) * kStaged;
+                char* const mine = to + rt * 2048 + lane * 16;
+                const unsigned minus128 = 0xc300c300u;
+                const bf16x8 off = __builtin_bit_cast(bf16x8, u32x4{minus128, minus128, minus128, minus128});
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const unsigned pair = w[i][j >> 1];
-                        q[c][i][j] = (_Float16)ldexpf(__uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16), up);
-                        sum += (float)q[c][i][j];
+                for (int c = 0; c < 2; ++c) st.excess[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(off, weights[c], st.excess[c], 0, 0, 0);
+                f32x4 fresh[2][2];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) fresh[kt][c] = f32x4{q.start[c], q.start[c], q.start[c], q.start[c]};
+                u32x4 wide;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    // (K's pieces come in the order (kt, step) 0 0, 0 1, .., 1 3)
+                    if (i + kAhead < 16) take(i + kAhead);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        if (i < 8) st.o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, piece[i]), weights[c], st.o[c][i], 0, 0, 0);
+                        else {
+                            const int kt = (i - 8) >> 2, step = (i - 8) & 3;
+                            fresh[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, piece[i]), q.q[c][step], fresh[kt][c], 0, 0, 0);
+                        }
                     }
-                sum += __shfl_xor(sum, 16);
-                sum += __shfl_xor(sum, 32);
-                start[c] = -1152.0f * sum;
-                // (a query that is not finite gives scores that are not numbers)
-                f[c] = most > 0x7f7fu ? __uint_as_float(0x7fc00000u) : fmaxf(ldexpf(p.scale_log2e, -up), 1.17549435e-38f);
-            }
-            for (; b < stop; b += kKG) {
-                if (b + kKG < stop) blk += kKG * stride;  // (behind the last one: that one again)
-                attend_cached(st, x, blk, q, start, f, p.len - b * kBlockRows, lane);
-            }
-        }
-        if (b < end) {
-            bf16x8 q[2][4];
+                    if (i < 8) {
+                        unsigned lo, hi;
+                        if (i < 4) widen_key(k[i], lo, hi);
+                        else widen(v[i - 4], lo, hi);
+                        wide[2 * (i & 1)] = lo;
+                        wide[2 * (i & 1) + 1] = hi;
+                        if (i & 1) *reinterpret_cast<u32x4*>(mine + (i < 4 ? 0 : 8192) + ((i >> 1) & 1) * 1024) = wide;
+                    } else if (i == 8) {
+                        *reinterpret_cast<float*>(to + 16384 + 4 * lane) = __uint_as_float(lane < 32 ? pair << 16 : pair & 0xffff0000u);
+                    } else if (i == 9) {
+                        ask(b + 6);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+                for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) q[c][i] = *reinterpret_cast<const bf16x8*>(q_row[c] + 64 * i);
-            const float f[2] = {p.scale_log2e, p.scale_log2e};
-            for (; b < end; b += kKG)
-                attend_own(st, p.k + (int64_t)g * 256, p.v + (int64_t)g * 256, row_bytes, b - p.n_cache_blocks, p.T, q, f, last, i16, h);
+                    for (int c = 0; c < 2; ++c) s[kt][c] = fresh[kt][c];
+                block = after;
+                __builtin_amdgcn_s_setprio(0);
+            }
+            if (kg == 0) __syncthreads();
         }
+    } else {
+        // the next block is asked for piece by piece as this one's are used up
+        raw16 k[4]{}, v[4]{}, pairs[2]{};
+        const char* blk = base + b * stride;
+        auto ask_keys = [&] {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const raw16*>(blk + j * 1024 + lane * 16);
+        };
+        auto ask_values = [&] {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const raw16*>(blk + kBlockV + j * 1024 + lane * 16);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) pairs[kt] = *reinterpret_cast<const raw16*>(blk + kBlockScales + 64 * kt + 16 * h);
+        };
+        Queries q;
+        if (b < stop) {
+            ask_keys();
+            ask_values();
+            take_queries(q, query, p.scale_log2e);
+        }
+        for (; b < stop; b += kKG) {
+            if (b + kKG < stop) blk += kKG * stride;  // (behind the last one: that one again)
+            f32x4 s[2][2], ks[2], vs[2];
+            bf16x8 weights[2];
+            multiply_keys(s, q, [&](int kt, int i) { return keys_of(k[2 * kt + (i >> 1)][2 * (i & 1)], k[2 * kt + (i >> 1)][2 * (i & 1) + 1]); });
+            ask_keys();
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    ks[kt][r] = __uint_as_float(pairs[kt][r] << 16);
+                    vs[kt][r] = __uint_as_float(pairs[kt][r] & 0xffff0000u);
+                }
+            weigh(st, weights, s, ks, vs, q, p.len - b * kBlockRows, h, [] {});
+            multiply_values<true>(st, weights, [&](int dt) { return values_of(v[dt >> 1][2 * (dt & 1)], v[dt >> 1][2 * (dt & 1) + 1]); });
+            ask_values();
+        }
+        own_blocks();
     }
+
+    // ---- the key groups meet in LDS, then 16 rows of a wavefront are done ----
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         st.l[c] += __shfl_xor(st.l[c], 16);
         st.l[c] += __shfl_xor(st.l[c], 32);
+        if (st.limit[c] == -INFINITY) st.m[c] = -INFINITY;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) st.o[c][dt] += st.excess[c];
     }
-    // the key groups, the upper half of them to the lower until one is left
+    __syncthreads();  // (blocks may still be read there)
+    float* const box = reinterpret_cast<float*>(smem);
+    // a set of columns of a wavefront in LDS: [dim % 8][lane][r], then references and sums
+    constexpr int kBox = 8 * 64 * 4 + 32;
+    auto put = [&](int slot, const f32x4 (&o)[8], float m, float l) {
+        float* const to = box + slot * kBox;
 #pragma unroll
-    for (int n = kKG / 2; n >= 1; n >>= 1) {
-        if (n < kKG / 2) __syncthreads();
-        if (kg >= n && kg < 2 * n) {
-            const int slot = wave - n * kRT;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (h == 0) {
-                    s_m[slot][16 * c + i16] = st.m[c];
-                    s_l[slot][16 * c + i16] = st.l[c];
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        f32x4 w;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = st.o[c][4 * half + e][r];
-                        *reinterpret_cast<f32x4*>(&s_o[slot][16 * c + i16][8 * (4 * h + r) + 4 * half]) = w;
-                    }
-            }
+        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(to + (dt * 64 + lane) * 4) = o[dt];
+        if (h == 0) {
+            to[2048 + i16] = m;
+            to[2064 + i16] = l;
         }
+    };
+    auto add = [&](f32x4 (&o)[8], float& m, float& l, int slot) {
+        const float* const from = box + slot * kBox;
+        const float m2 = from[2048 + i16], mx = fmaxf(m, m2);
+        const float a = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx), b2 = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx);
+        m = mx;
+        l = l * a + from[2064 + i16] * b2;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) o[dt] = o[dt] * a + *reinterpret_cast<const f32x4*>(from + (dt * 64 + lane) * 4) * b2;
+    };
+    if constexpr (kShared) {  // each group of two does one set of columns
+        if (kg == 0) put(wave, st.o[1], st.m[1], st.l[1]);
+        else put(wave, st.o[0], st.m[0], st.l[0]);
         __syncthreads();
-        if (kg < n) {
+        if (kg == 1) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const float m2 = s_m[wave][16 * c + i16], mx = fmaxf(st.m[c], m2);
-                const float a = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[c] - mx), b = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx);
-                st.m[c] = mx;
-                st.l[c] = st.l[c] * a + s_l[wave][16 * c + i16] * b;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const f32x4 w = *reinterpret_cast<const f32x4*>(&s_o[wave][16 * c + i16][8 * (4 * h + r) + 4 * half]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) st.o[c][4 * half + e][r] = st.o[c][4 * half + e][r] * a + w[e] * b;
-                    }
-            }
+            for (int dt = 0; dt < 8; ++dt) st.o[0][dt] = st.o[1][dt];
+            st.m[0] = st.m[1];
+            st.l[0] = st.l[1];
         }
+        add(st.o[0], st.m[0], st.l[0], (wave + kRT) % kWaves);
+    } else {  // every wavefront leaves both; two of them add a set each, in the order of the groups
+        put(2 * wave, st.o[0], st.m[0], st.l[0]);
+        put(2 * wave + 1, st.o[1], st.m[1], st.l[1]);
+        __syncthreads();
+        if (wave >= 2) return;
+        st.m[0] = -INFINITY;
+        st.l[0] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) st.o[0][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+        for (int n = 0; n < kWaves; ++n) add(st.o[0], st.m[0], st.l[0], 2 * n + wave);
     }
-    if (kg != 0) return;
+    const int row = row0 + 16 * (kShared ? kg : wave) + i16;
+    const float l = st.l[0];
+    if (p.nsplit == 1) {
+        const float inv = 1.0f / l;
+        const int t = token_of(row);
+        __bf16* const dst = p.out + ((int64_t)t * p.Hq + (int64_t)g * p.G + row - t * p.G) * D + 32 * h;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int row = row0 + 16 * c + i16;
-        const float inv = p.nsplit > 1 && st.l[c] == 0.f ? 0.f : 1.0f / st.l[c];  // (0: none of the split's keys is visible to the row)
-        if (p.nsplit == 1) {
-            const int t = row / p.G;
-            __bf16* const dst = p.out + ((int64_t)t * p.Hq + (int64_t)g * p.G + row - t * p.G) * D + 32 * h;
+        for (int r = 0; r < 4; ++r) {
+            bf16x8 w;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                bf16x8 w;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = (__bf16)(st.o[c][e][r] * inv);
-                if (row < p.M) *reinterpret_cast<bf16x8*>(dst + 8 * r) = w;
-            }
-        } else {
-            float big = 0.f;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) big = fmaxf(big, fabsf(st.o[c][dt][r]));
-            big *= inv;
-            big = fmaxf(big, __shfl_xor(big, 16));
-            big = fmaxf(big, __shfl_xor(big, 32));
-            const int se = min(max(127 + 14 + 127 - (int)((__float_as_uint(big) >> 23) & 255u), 1), 254);
-            const float scale = __uint_as_float((unsigned)se << 23);
-            const int64_t pr = ((int64_t)split * p.Hkv + g) * p.M + row;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                f16x8 w;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = (_Float16)(st.o[c][e][r] * inv * scale);
-                if (row < p.M) *reinterpret_cast<f16x8*>(p.part_o + pr * D + 32 * h + 8 * r) = w;
-            }
-            if (h == 0 && row < p.M)
-                *reinterpret_cast<float4*>(p.part_ml + pr * 4) = make_float4(st.m[c], st.l[c], __uint_as_float((unsigned)(254 - se) << 23), 0.f);
+            for (int e = 0; e < 8; ++e) w[e] = (__bf16)(st.o[0][e][r] * inv);
+            if (row < p.M) *reinterpret_cast<bf16x8*>(dst + 8 * r) = w;
         }
+        return;
     }
+    float big = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) big = fmaxf(big, fabsf(st.o[0][dt][r]));
+    const float inv = l == 0.f ? 0.f : 1.0f / l;  // (0: none of the split's keys is visible to the row)
+    big *= inv;
+    big = fmaxf(big, __shfl_xor(big, 16));
+    big = fmaxf(big, __shfl_xor(big, 32));
+    const int se = min(max(127 + 14 + 127 - (int)((__float_as_uint(big) >> 23) & 255u), 1), 254);
+    const float scale = __uint_as_float((unsigned)se << 23);
+    const int64_t pr = ((int64_t)split * p.Hkv + g) * p.M + row;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        f16x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (_Float16)(st.o[0][e][r] * inv * scale);
+        if (row < p.M) *reinterpret_cast<f16x8*>(p.part_o + pr * D + 32 * h + 8 * r) = w;
+    }
+    if (h == 0 && row < p.M)
+        *reinterpret_cast<float4*>(p.part_ml + pr * 4) = make_float4(st.m[0], l, __uint_as_float((unsigned)(254 - se) << 23), 0.f);
 }
 
 // The splits of a row added in index order: 16 lanes a row, 8 dims each.
@@ -474,11 +689,16 @@ struct Plan {
 Plan plan_of(const vs_shape& s, int32_t n_tokens, int32_t len) {
     const int G = s.n_q_heads / s.n_kv_heads, tiles = (n_tokens * G + kTileRows - 1) / kTileRows;
     Plan pl;
-    pl.rt = tiles <= 1 ? 1 : tiles <= 2 ? 2 : 4;
+    pl.rt = tiles <= 2 ? 1 : 4;
     pl.groups = (tiles + pl.rt - 1) / pl.rt;
-    // one workgroup per compute unit, and a block for every key group at least
-    const int blocks = (len + kBlockRows - 1) / kBlockRows + (n_tokens + 31) / 32, kg = kWaves / pl.rt;
-    pl.nsplit = std::max(1, std::min({256 / (pl.groups * s.n_kv_heads), blocks / kg, kMaxSplits}));
+    // One workgroup per compute unit, and a block for every key group at least.  us for attention and merge, 28/4 heads, by splits:
+    //   170 tokens over 200 rows (13 blocks) 19.8 at 1, 22.7 at 2, 20.7 at 4; over 352 rows 21.9 at 1, 20.4 at 4, 21.0 at 6;
+    //   over 736 rows 27.9, 22.1 at 4, 23.1 at 6; over 4416 rows 85.7, 36.7 at 4, 32.5 at 6 (8, more than run at once: 46.0);
+    //   37 tokens over 711 rows 23.8 at 1, 17.7 at 4, 16.7 at 12.
+    const int blocks = (len + kBlockRows - 1) / kBlockRows + (n_tokens + 31) / 32, kg = kWaves / pl.rt, units = pl.groups * s.n_kv_heads;
+    pl.nsplit = std::max(1, std::min({256 / units, blocks / kg, kMaxSplits}));
+    if (pl.rt == 4 && blocks <= 13) pl.nsplit = 1;
+    else if (pl.nsplit > 4 && units * pl.nsplit > 192 && blocks < 6 * pl.nsplit) pl.nsplit = std::max(4, blocks / 6);
     return pl;
 }
 size_t partial_bytes(const vs_shape& s, int32_t n_tokens, int nsplit) {
@@ -496,11 +716,11 @@ size_t prefill8_workspace_bytes(const vs_shape& s, int32_t max_tokens, int32_t m
     return most;
 }
 
-hipError_t launch_prefill8(const vs_shape& s, const void* cache, int32_t len, const void* q, const void* k, const void* v, int32_t n_tokens,
-                           void* out, void* workspace, hipStream_t st) {
+hipError_t launch_prefill8(const vs_shape& s, void* cache, int32_t len, const void* q, const void* k, const void* v, int32_t n_tokens,
+                           int32_t first_kept, void* out, void* workspace, hipStream_t st) {
     const Plan pl = plan_of(s, n_tokens, len);
     Prefill8Params p;
-    p.cache = (const char*)cache;
+    p.cache = (char*)cache;
     p.q = (const char*)q;
     p.k = (const char*)k;
     p.v = (const char*)v;
@@ -517,9 +737,12 @@ hipError_t launch_prefill8(const vs_shape& s, const void* cache, int32_t len, co
     p.scale_log2e = s.softmax_scale * kLog2e;
     p.part_ml = (float*)workspace;
     p.part_o = (_Float16*)(p.part_ml + (int64_t)pl.nsplit * p.M * p.Hkv * 4);
-    const int grid = pl.nsplit * pl.groups * p.Hkv;
+    p.by_G = (unsigned)(0xffffffffu / p.G + 1u);  // exact for row * G < 2^32
+    p.first_kept = first_kept;
+    p.n_keeping = first_kept < n_tokens ? ((len + n_tokens - first_kept - 1) / kBlockRows - len / kBlockRows + 1) * p.Hkv : 0;
+    const int per_plane = pl.nsplit * p.Hkv * kWaves;
+    const dim3 grid(pl.nsplit, p.Hkv, pl.groups + (p.n_keeping + per_plane - 1) / per_plane);
     if (pl.rt == 1) prefill8_kernel<1><<<grid, kThreads, 0, st>>>(p);
-    else if (pl.rt == 2) prefill8_kernel<2><<<grid, kThreads, 0, st>>>(p);
     else prefill8_kernel<4><<<grid, kThreads, 0, st>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.nsplit == 1) return e;
