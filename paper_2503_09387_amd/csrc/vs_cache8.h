@@ -102,7 +102,12 @@ __device__ __forceinline__ unsigned quantise(const raw16& k, const raw16& v, uin
 // maximum is four exchanges among 16 lanes, and a lane ends up with all 8 keys that its V operand has side by side.
 __device__ __forceinline__ void write_block(char* blk, const char* k, const char* v, int64_t row_bytes, int row0, int at, int end, int lane) {
     const int c = lane & 15, h = lane >> 4;
-    raw16 kx[8], vx[8];
+    raw16 kx[8], vx[8], was[4];
+    // what other rows have among this lane's V codes goes back as it was (nobody else writes to the block meanwhile)
+    const bool whole = at <= row0 && end >= row0 + kBlockRows;
+    if (!whole)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) was[j] = *reinterpret_cast<const raw16*>(blk + kBlockV + j * 1024 + lane * 16);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
         const int first = row0 + 16 * (u >> 2) + (u & 3);  // of four rows, 4 apart
@@ -111,44 +116,33 @@ __device__ __forceinline__ void write_block(char* blk, const char* k, const char
         kx[u] = *reinterpret_cast<const raw16*>(k + off);
         vx[u] = *reinterpret_cast<const raw16*>(v + off);
     }
-    unsigned codes[8][8];
-    bool all = true;
+    unsigned codes[8][8], mask[2] = {0u, 0u};
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
         const int first = row0 + 16 * (u >> 2) + (u & 3), key = 16 * (u >> 2) + 4 * h + (u & 3), row = row0 + key;
         if (first + 12 < at || first >= end) {
-            all = false;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) codes[u][j] = 0;
             continue;
         }
-        const bool mine = row >= at && row < end;
-        all = all && mine;
         uint2 k_codes;
         const unsigned pair = quantise(kx[u], vx[u], k_codes, codes[u]);
-        if (mine) {
+        if (row >= at && row < end) {
+            mask[u >> 2] |= 0xffu << (8 * (u & 3));
             *reinterpret_cast<uint2*>(blk + k_code_offset(key, c)) = k_codes;
             if (c == 0) *reinterpret_cast<unsigned*>(blk + kBlockScales + 4 * key) = pair;
         }
     }
-    if (all) {
 #pragma unroll
-        for (int dt = 0; dt < 8; dt += 2) {
-            raw16 w;
+    for (int dt = 0; dt < 8; dt += 2) {
+        raw16 w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = dt + (i >> 1), u = 4 * (i & 1);
-                w[i] = bytes_of(codes[u][d], codes[u + 1][d], codes[u + 2][d], codes[u + 3][d]);
-            }
-            *reinterpret_cast<raw16*>(blk + kBlockV + (dt >> 1) * 1024 + lane * 16) = w;
+        for (int i = 0; i < 4; ++i) {
+            const int d = dt + (i >> 1), u = 4 * (i & 1);
+            w[i] = bytes_of(codes[u][d], codes[u + 1][d], codes[u + 2][d], codes[u + 3][d]);
+            if (!whole) w[i] = (w[i] & mask[i & 1]) | (was[dt >> 1][i] & ~mask[i & 1]);
         }
-    } else {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int first = row0 + 16 * (u >> 2) + (u & 3), key = 16 * (u >> 2) + 4 * h + (u & 3), row = row0 + key;
-            if (first + 12 < at || first >= end) continue;
-            if (row >= at && row < end)
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt) blk[v_code_offset(key, c, dt)] = (char)codes[u][dt];
-        }
+        *reinterpret_cast<raw16*>(blk + kBlockV + (dt >> 1) * 1024 + lane * 16) = w;
     }
 }
 
@@ -160,9 +154,10 @@ hipError_t launch_cache8_append(const vs_shape& s, int32_t n_caches, void* slab,
 hipError_t launch_cache8_read(const vs_shape& s, int32_t n_caches, const void* slab, int32_t capacity, const LenTable& first, int32_t n_rows,
                               void* k_out, void* v_out, hipStream_t st);
 // lens: valid rows, the appended row included.
+// counters: the arrival counters of decoding steps at the front of a workspace's control block (see launch_decode_mfma).
 size_t decode8_workspace_bytes(const vs_shape& s, int32_t n_streams);
 hipError_t launch_decode8(const vs_shape& s, int32_t n_streams, void* slab, int32_t capacity, const LenTable& lens, const void* q,
-                          const void* k_new, const void* v_new, void* out, void* workspace, hipStream_t st);
+                          const void* k_new, const void* v_new, void* out, void* counters, void* workspace, hipStream_t st);
 // A run's n_tokens over the len rows of one cache and over one another.  Workspace: prefill8_workspace_need; prefill8_workspace_bytes for any run within
 // limits.
 size_t prefill8_workspace_need(const vs_shape& s, int32_t n_tokens, int32_t len);

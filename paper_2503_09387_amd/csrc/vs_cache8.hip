@@ -223,7 +223,7 @@ vs_status vs_cache8_decode_attn(const vs_shape* shape, int32_t n_streams, void* 
         for (int32_t i = 0; i < n; ++i) t.v[i] = lens[i0 + i] + add;
         if (launch_decode8(*shape, n, static_cast<char*>(slab) + i0 * bytes, capacity, t, static_cast<const char*>(q) + i0 * qb,
                            add ? static_cast<const char*>(k_new) + i0 * rb : nullptr, add ? static_cast<const char*>(v_new) + i0 * rb : nullptr,
-                           static_cast<char*>(out) + i0 * qb, static_cast<char*>(workspace) + ctrl, static_cast<hipStream_t>(hip_stream)) !=
+                           static_cast<char*>(out) + i0 * qb, workspace, static_cast<char*>(workspace) + ctrl, static_cast<hipStream_t>(hip_stream)) !=
             hipSuccess)
             return VS_ERR_HIP;
         for (int32_t i = 0; i < n; ++i) lens[i0 + i] += add;

@@ -1,32 +1,17 @@
 // Prefill attention over a cache in 8 bits (Eq. 1 of Section 3.1; Section 3.3): a run's tokens over the retained rows and, causally, over
-// one another.
-//
-//   score(key) = (q . k_codes) * s_k * scale,   out = sum_key p(key) s_v(key) v_codes / sum_key p(key);   scales 1 for the run's own rows
-//
-// As in the decoding step the products take codes, and the scales of rows go to the scores and the probabilities:
-//   * q . (k_codes + 1152): a code + 128 becomes an fp16 by putting 0x64 before its byte (1024 + byte: one permutation for two values);
-//     the query is an fp16 after the power of two that brings its largest entry into [2^14, 2^15), which loses nothing down to 2^-28
-//     of that entry and 2^-39 of it below; the sums start at -1152 sum q.
-//   * p s_v in bf16 (8 bits, as P does over caches in bf16; the denominator sums p before that) times the codes + 128 in bf16, which
-//     loses nothing, less 128 times the sum of p s_v, through one more product.
-// The G query heads of a KV head are packed into rows (row = token * G + head).  A wavefront holds 32 rows (two sets of 16 columns) and walks
+// one another.  The arithmetic is in vs_cache8_attn.h.  The G query heads of a KV head are packed into rows (row = token * G + head).  A wavefront holds 32 rows (two sets of 16 columns) and walks
 // blocks of 32 keys.  A workgroup is 8 wavefronts, kRT row tiles x 8 / kRT key groups, which are added in LDS at the end:
 //   * kRT = 4: two key groups, a wavefront of each on every SIMD.  A block comes from memory once, a quarter by each wavefront of
 //     its group, which widens its quarter into LDS for all four (widening costs as many vector instructions as the softmax of 32 rows).
 //     The groups take turns, a barrier apart: while one multiplies (the last block's values, the next one's keys), the other works out
 //     probabilities and widens, so that matrix and vector instructions of a SIMD run side by side.
 //   * kRT = 1, for up to 64 rows: every wavefront has a block of its own, straight from memory into the multiplier.
-#include "vs_cache8.h"
+#include "vs_cache8_attn.h"
 
 #include <algorithm>
 
 namespace vs {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int D = 128;
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
@@ -60,95 +45,6 @@ struct State {
     float m[2], l[2];  // reference (log2 units; 0 until a key has been seen), this lane's share of the sum
     float limit[2];    // how far scores may pass the reference before it is refreshed: -INFINITY until a key has been seen
 };
-
-// (fmaxf of values that come out of a selection is three instructions for one)
-__device__ __forceinline__ float max_of_8(const float (&z)[8]) {
-    float a, b;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(z[0]), "v"(z[1]), "v"(z[2]));
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(z[3]), "v"(z[4]), "v"(z[5]));
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(z[6]), "v"(z[7]), "v"(a));
-    asm("v_max_f32 %0, %1, %2" : "=v"(a) : "v"(a), "v"(b));
-    return a;
-}
-
-// four codes of V as bf16: whole numbers 0..255, whose fp32 has nothing in its lower half
-__device__ __forceinline__ void widen(unsigned w, unsigned& lo, unsigned& hi) {
-    const unsigned a = __float_as_uint((float)(w & 255u)), b = __float_as_uint((float)((w >> 8) & 255u));
-    const unsigned c = __float_as_uint((float)((w >> 16) & 255u)), d = __float_as_uint((float)(w >> 24));
-    lo = __builtin_amdgcn_perm(b, a, 0x07060302u);
-    hi = __builtin_amdgcn_perm(d, c, 0x07060302u);
-}
-
-// The queries of a wavefront's columns as fp16, what the sums over codes + 1152 start at, and the factor of the scores.
-struct Queries {
-    f16x8 q[2][4];
-    float start[2], f[2];
-};
-__device__ __forceinline__ void take_queries(Queries& out, const raw16 (&w)[2][4], float scale_log2e) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        unsigned most = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) most = max_pairs(most, w[c][i][j] & 0x7fff7fffu);
-        most = max(most & 0xffffu, most >> 16);
-        most = max(most, (unsigned)__shfl_xor((int)most, 16));
-        most = max(most, (unsigned)__shfl_xor((int)most, 32));
-        // (up to 2^126: the smallest bf16 is then 2^-7, an fp16 like any other)
-        const int up = min(14 + 127 - (int)(most >> 7), 126);
-        const float factor = __uint_as_float((unsigned)(127 + up) << 23);
-        const unsigned minus1152 = 0xe480e480u;
-        const f16x8 off = __builtin_bit_cast(f16x8, u32x4{minus1152, minus1152, minus1152, minus1152});
-        f32x4 start = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned pair = w[c][i][j >> 1];
-                out.q[c][i][j] = (_Float16)(__uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16) * factor);
-            }
-            start = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, out.q[c][i], start, 0, 0, 0);
-        }
-        out.start[c] = start[0];
-        // (a query that is not finite gives scores that are not numbers; a factor of 0 would make them of what is masked)
-        out.f[c] = most > 0x7f7fu ? __uint_as_float(0x7fc00000u) : fmaxf(ldexpf(scale_log2e, -up), 1.17549435e-38f);
-    }
-}
-
-// four codes of K as fp16, 1152 too large
-__device__ __forceinline__ void widen_key(unsigned w, unsigned& lo, unsigned& hi) {
-    w ^= 0x80808080u;
-    lo = __builtin_amdgcn_perm(0x64646464u, w, 0x05010400u);
-    hi = __builtin_amdgcn_perm(0x64646464u, w, 0x07030602u);
-}
-__device__ __forceinline__ f16x8 keys_of(unsigned x, unsigned y) {
-    u32x4 a;
-    unsigned lo, hi;
-    widen_key(x, lo, hi);
-    a[0] = lo, a[1] = hi;
-    widen_key(y, lo, hi);
-    a[2] = lo, a[3] = hi;
-    return __builtin_bit_cast(f16x8, a);
-}
-// 8 V codes + 128 as bf16
-__device__ __forceinline__ bf16x8 values_of(unsigned x, unsigned y) {
-    u32x4 a;
-    unsigned lo, hi;
-    widen(x, lo, hi);
-    a[0] = lo, a[1] = hi;
-    widen(y, lo, hi);
-    a[2] = lo, a[3] = hi;
-    return __builtin_bit_cast(bf16x8, a);
-}
-
-// x *= f in the registers where x is: written as products, the compiler gives the sums other registers behind the branch around
-// them, and copies them on every turn.
-__device__ __forceinline__ void scale_in_place(f32x4& x, float f) {
-    float a = x[0], b = x[1], c = x[2], d = x[3];
-    asm volatile("v_mul_f32 %0, %0, %4\n\tv_mul_f32 %1, %1, %4\n\tv_mul_f32 %2, %2, %4\n\tv_mul_f32 %3, %3, %4" : "+v"(a), "+v"(b), "+v"(c), "+v"(d) : "v"(f));
-    x = f32x4{a, b, c, d};
-}
 
 // Scores less the reference become probabilities; the sums take them.
 __device__ __forceinline__ void soften(State& st, float (&x)[2][8]) {
@@ -184,23 +80,23 @@ __device__ __forceinline__ void soften(State& st, float (&x)[2][8]) {
 
 // The three steps of a block of cached rows.  Scores of its keys (k_of(kt, i): 16 keys, 32 dims):
 template <typename KOf>
-__device__ __forceinline__ void multiply_keys(f32x4 (&s)[2][2], const Queries& q, KOf k_of) {
+__device__ __forceinline__ void multiply_keys(f32x4 (&s)[2][2], const Queries (&q)[2], KOf k_of) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) s[kt][c] = f32x4{q.start[c], q.start[c], q.start[c], q.start[c]};
+        for (int c = 0; c < 2; ++c) s[kt][c] = f32x4{q[c].start, q[c].start, q[c].start, q[c].start};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             const f16x8 k = k_of(kt, i);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) s[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q.q[c][i], s[kt][c], 0, 0, 0);
+            for (int c = 0; c < 2; ++c) s[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[c].q[i], s[kt][c], 0, 0, 0);
         }
 }
 // probabilities times the scales of V, of the first `valid` rows:
 template <typename Then>
-__device__ __forceinline__ void weigh(State& st, bf16x8 (&p)[2], const f32x4 (&s)[2][2], const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Queries& q,
+__device__ __forceinline__ void weigh(State& st, bf16x8 (&p)[2], const f32x4 (&s)[2][2], const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Queries (&q)[2],
                                       int valid, int h, Then then) {
     float x[2][8], v[8];
 #pragma unroll
@@ -208,7 +104,7 @@ __device__ __forceinline__ void weigh(State& st, bf16x8 (&p)[2], const f32x4 (&s
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) x[c][4 * kt + r] = fmaf(s[kt][c][r], ks[kt][r] * q.f[c], -st.m[c]);
+            for (int c = 0; c < 2; ++c) x[c][4 * kt + r] = fmaf(s[kt][c][r], ks[kt][r] * q[c].f, -st.m[c]);
             v[4 * kt + r] = vs[kt][r];
         }
     if (valid < kBlockRows) {
@@ -423,8 +319,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         }
         own_blocks();  // (first: their queries are there as they are needed, and the cache's first blocks come meanwhile)
         if (first < stop) {
-            Queries q;
-            take_queries(q, query, p.scale_log2e);
+            const Queries q[2] = {queries_of(query[0], p.scale_log2e), queries_of(query[1], p.scale_log2e)};
             widen_into(0);
             k = k1, v = v1, pair = pair1;
             __syncthreads();
@@ -470,7 +365,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) fresh[kt][c] = f32x4{q.start[c], q.start[c], q.start[c], q.start[c]};
+                    for (int c = 0; c < 2; ++c) fresh[kt][c] = f32x4{q[c].start, q[c].start, q[c].start, q[c].start};
                 u32x4 wide;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -481,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
                         if (i < 8) st.o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, piece[i]), weights[c], st.o[c][i], 0, 0, 0);
                         else {
                             const int kt = (i - 8) >> 2, step = (i - 8) & 3;
-                            fresh[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, piece[i]), q.q[c][step], fresh[kt][c], 0, 0, 0);
+                            fresh[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, piece[i]), q[c].q[step], fresh[kt][c], 0, 0, 0);
                         }
                     }
                     if (i < 8) {
@@ -521,11 +416,12 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) pairs[kt] = *reinterpret_cast<const raw16*>(blk + kBlockScales + 64 * kt + 16 * h);
         };
-        Queries q;
+        Queries q[2];
         if (b < stop) {
             ask_keys();
             ask_values();
-            take_queries(q, query, p.scale_log2e);
+            q[0] = queries_of(query[0], p.scale_log2e);
+            q[1] = queries_of(query[1], p.scale_log2e);
         }
         for (; b < stop; b += kKG) {
             if (b + kKG < stop) blk += kKG * stride;  // (behind the last one: that one again)

@@ -35,9 +35,10 @@ def attend(q, k, v, seen, scale):
 
 def decode_bound(q, k, v, ref, absolute, most, scale):
     """How far a value of a decoding step over rows in 8 bits may be off, q [Hq][D], k [L][Hkv][D] (what the rows stand for), v likewise.
-    * the query in whole numbers of 16 bits: each entry at most 2^-15 of the largest off (half a step, or the one step that the
-      largest number of 8 bits gives up), so a score at most e = 2^-15 max|q| sum|k| scale, and 2^-21 of itself by the fp32 arithmetic
-      around the whole sums (four roundings) and the exponential; a weight then by a factor of exp(2 e) at most, on top
+    * sums of (code + 1152) q over 128 dims in fp32 that start at -1152 sum q: what has come together is at most 1280 sum|q| s, s at most
+      max|k| / 126, and rounded to 2^-24 of that by each of 16 additions of eight products and what they start at: a score at most
+      e = 2^-24 17 (1280 / 126) sum|q| max|k| scale < 2^-16.5 of the rest (the query in fp16 gives up 2^-39 of its largest entry, far
+      less), and four roundings and the exponential of fp32 2^-21 of itself; a weight then by a factor of exp(2 e) at most, on top
       and below the fraction; and whatever the weights are, they are fractions of one: no value leaves the range of the keys' values, so it is
       at most twice the largest of their magnitudes off (which is less where scores are large: e grows with them);
     * a probability below 2^-126 may be 0 in fp32, beside a sum of at least 1 (the reference never passes the largest score): at most
@@ -46,11 +47,10 @@ def decode_bound(q, k, v, ref, absolute, most, scale):
     * sums of p s (code + 128), up to 255 p s each where max|v| is over 126 / 127 * 127 p s: an fp32 rounding per 32 keys of what
       has come together (2^-24 of at most 2.02 * 2 sum p max|v|), and as many for what is taken off."""
     g = q.shape[0] // k.shape[1]
-    sums = np.abs(k).sum(-1).max(0)                                     # [Hkv]
-    e = 2.0 ** -15 * np.abs(q).max(-1) * np.repeat(sums, g) * scale     # [Hq]
-    z = np.abs(q).sum(-1) * np.repeat(np.abs(k).max((0, 2)), g) * scale * 2.0 ** -21 + 2.0 ** -21
+    z = np.abs(q).sum(-1) * np.repeat(np.abs(k).max((0, 2)), g) * scale  # [Hq]
+    e = 2.0 ** -16.5 * z + 2.0 ** -21 * (z + 1.0)
     with np.errstate(over="ignore", invalid="ignore"):
-        weights = np.fmin(np.expm1(2.0 * (e + z))[:, None] * 1.01 * absolute, 2.0 * np.repeat(np.abs(v).max(0), g, 0))
+        weights = np.fmin(np.expm1(2.0 * e)[:, None] * 1.01 * absolute, 2.0 * np.repeat(np.abs(v).max(0), g, 0))
     steps = k.shape[0] // 32 + 8
     return 2.0 ** -8 * np.abs(ref) + 2.0 ** -8 * 1.01 * absolute + weights + 2.0 ** -24 * steps * 8.1 * most + 2.0 ** -126 * np.repeat(np.abs(v).sum(0), g, 0)
 
