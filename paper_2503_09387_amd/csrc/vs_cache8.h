@@ -37,15 +37,36 @@ __device__ __forceinline__ int v_code_offset(int key, int c, int dt) {
     return kBlockV + (dt >> 1) * 1024 + (((key & 15) >> 2) * 16 + c) * 16 + (dt & 1) * 8 + (key >> 4) * 4 + (key & 3);
 }
 
+// Exchanges in registers (through LDS each would take some 130 cycles): the value of the lane N places on among the 16 of a row,
+// and the largest, or the sum, over the lanes 16 and 32 apart.
+template <int N>
+__device__ __forceinline__ unsigned turned(unsigned x) {
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xf, 0xf, false);  // row_ror
+}
+template <typename Op>
+__device__ __forceinline__ unsigned over_rows(unsigned x, Op op) {
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = op(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return op(b[0], b[1]);
+}
+__device__ __forceinline__ float max_over_rows(float x) {
+    return __uint_as_float(over_rows(__float_as_uint(x), [](unsigned a, unsigned b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+__device__ __forceinline__ float sum_over_rows(float x) {
+    return __uint_as_float(over_rows(__float_as_uint(x), [](unsigned a, unsigned b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+
 // The larger magnitudes of two pairs of bf16 bit patterns without their signs (K below, V above): as whole numbers they are
 // ordered as the values are, with infinities and then NaN above all.
 __device__ __forceinline__ unsigned max_pairs(unsigned a, unsigned b) {
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
-// The scale's bf16 pattern for the largest magnitude's.
+// The scale's bf16 pattern for the largest magnitude's.  (a / 127 to a rounding, and exactly where it is a number of 8 bits: see Divisor.)
 __device__ __forceinline__ unsigned scale_bits(unsigned most) {
-    const unsigned up = (__float_as_uint(__uint_as_float(most << 16) / 127.0f) + 0xffffu) >> 16;
+    const float a = __uint_as_float(most << 16), t = a * (1.0f / 127.0f);
+    const unsigned up = (__float_as_uint(fmaf(fmaf(-t, 127.0f, a), 1.0f / 127.0f, t)) + 0xffffu) >> 16;
     return most > 0x7f7fu ? 0x7fc0u : max(up, 0x80u);
 }
 // The largest magnitudes among 8 K and 8 V values (16 bytes each) of this lane and the row's 15 others.
@@ -53,9 +74,10 @@ __device__ __forceinline__ unsigned row_most(const raw16& k, const raw16& v) {
     unsigned a = max_pairs(max_pairs(k[0] & 0x7fff7fffu, k[1] & 0x7fff7fffu), max_pairs(k[2] & 0x7fff7fffu, k[3] & 0x7fff7fffu));
     unsigned b = max_pairs(max_pairs(v[0] & 0x7fff7fffu, v[1] & 0x7fff7fffu), max_pairs(v[2] & 0x7fff7fffu, v[3] & 0x7fff7fffu));
     unsigned m = max_pairs(__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(b, a, 0x07060302u));
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) m = max_pairs(m, __shfl_xor(m, o));
-    return m;
+    m = max_pairs(m, turned<8>(m));
+    m = max_pairs(m, turned<4>(m));
+    m = max_pairs(m, turned<2>(m));
+    return max_pairs(m, turned<1>(m));
 }
 // Codes.  x / s to a rounding, or exactly where a product or a tie is: r = 1 / s to a rounding, then t = x r and what the remainder
 // x - t s adds.  (The division that the compiler writes takes twice the instructions.)  Below 2^-64 both go up by 2^64, where

@@ -75,8 +75,7 @@ __device__ __forceinline__ Queries queries_of(const raw16 (&w)[4], float scale_l
 #pragma unroll
         for (int j = 0; j < 4; ++j) most = max_pairs(most, w[i][j] & 0x7fff7fffu);
     most = max(most & 0xffffu, most >> 16);
-    most = max(most, (unsigned)__shfl_xor((int)most, 16));
-    most = max(most, (unsigned)__shfl_xor((int)most, 32));
+    most = over_rows(most, [](unsigned a, unsigned b) { return max(a, b); });
     // (up to 2^126: the smallest bf16 is then 2^-7, an fp16 like any other)
     const int up = min(14 + 127 - (int)(most >> 7), 126);
     const float factor = __uint_as_float((unsigned)(127 + up) << 23);

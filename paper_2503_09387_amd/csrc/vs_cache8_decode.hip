@@ -80,8 +80,7 @@ __device__ __forceinline__ void attend(State& st, const Block& b, const Queries&
     }
     float mx = max_of_8(z);
     if (__any(mx > st.m + kLazyMax)) {  // rare after the first block
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        mx = max_over_rows(mx);
         const float m_new = fmaxf(st.m, mx), alpha = __builtin_amdgcn_exp2f(st.m - m_new);  // 0 at first
         st.m = m_new;
         st.l *= alpha;
@@ -218,12 +217,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(Decode8Params p) {
         for (int i = 0; i < 4; ++i) words[i] = *reinterpret_cast<const raw16*>(q_row + 64 * i);
         // the step's new row, by the wavefront that attends over the block that it falls into: to memory, and into the block as it is here
         const bool keeps = p.k_new && end == n_blocks && wave == (unsigned)(n_blocks - 1 - first) % kWaves;
-        raw16 k_new{}, v_new{};
-        if (keeps) {
-            const int64_t at = ((int64_t)s * p.Hkv + g) * 256 + 16 * i16;
-            k_new = *reinterpret_cast<const raw16*>(p.k_new + at);
-            v_new = *reinterpret_cast<const raw16*>(p.v_new + at);
-        }
+        const int64_t at = ((int64_t)s * p.Hkv + g) * 256 + 16 * i16;  // (asked for by all: behind a branch it would be waited for)
+        const raw16 k_new = *reinterpret_cast<const raw16*>((p.k_new ? p.k_new : p.q) + at), v_new = *reinterpret_cast<const raw16*>((p.k_new ? p.v_new : p.q) + at);
         Block x, y;
         const char* blk = base + b * stride;
         fetch(x, blk, lane);
@@ -255,8 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(Decode8Params p) {
             if (b < end) turn(y);
         }
     }
-    st.l += __shfl_xor(st.l, 16);
-    st.l += __shfl_xor(st.l, 32);
+    st.l = sum_over_rows(st.l);
     if (h == 0) {
         s_m[wave][i16] = st.m;
         s_l[wave][i16] = st.l;
@@ -326,10 +320,15 @@ __global__ __launch_bounds__(64) void decode8_shares_kernel(Decode8Params p) {
 }
 
 constexpr int kMaxWorkgroups = 2048 / kWaves;
-constexpr int kMaxSharesInside = 12, kMaxBlocksInside = 80;
+constexpr int kMaxSharesInside = 12, kMaxBlocksInside = 80, kAloneBlocks = 16;
 
-// Blocks per share: the fewest, from a block per wavefront on, with which all shares run at once, a workgroup per compute unit.  Streams that
-// do not fit that way are not shared out.
+// Blocks per share.  us a step, 28/4 heads:
+//   * up to 16 blocks a stream (2 a wavefront) one share and no merge: 1 x 256 rows 6.1 (shares of 8: 7.0), 1 x 380 6.4 (8.0), 1 x 500 7.25 (8.0);
+//     beyond, shares: 1 x 700 8.6 as one and 8.0 in shares of 8;
+//   * the fewest, from a block per wavefront on, with which all shares run at once, a workgroup per compute unit;
+//   * but at most 12 shares, which the last to arrive adds, as long as they are no more than 80 blocks: 1 x 8192 12.3 (32 shares and a second
+//     launch 15.1), 1 x 16384 15.2 (19.9), 1 x 32768 22.8 (22.9), 1 x 50000 30.2 (25.1).
+// Streams that do not fit all at once are not shared out.
 int blocks_per_share(const LenTable& lens, int n_streams, int n_kv_heads) {
     auto blocks_of = [&](int i) { return (lens.v[i] + kBlockRows - 1) / kBlockRows; };
     int64_t total = 0;
@@ -338,7 +337,7 @@ int blocks_per_share(const LenTable& lens, int n_streams, int n_kv_heads) {
         total += blocks_of(i);
         most = std::max(most, blocks_of(i));
     }
-    if ((int64_t)n_streams * n_kv_heads >= kMaxWorkgroups) return most;
+    if (most <= kAloneBlocks || (int64_t)n_streams * n_kv_heads >= kMaxWorkgroups) return most;
     auto fits = [&](int c) {
         int64_t n = 0;
         for (int i = 0; i < n_streams; ++i) n += (blocks_of(i) + c - 1) / c;

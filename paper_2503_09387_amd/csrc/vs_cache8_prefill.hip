@@ -54,8 +54,7 @@ __device__ __forceinline__ void soften(State& st, float (&x)[2][8]) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const bool seen = st.limit[c] != -INFINITY;
-            float up = fmaxf(mx[c], __shfl_xor(mx[c], 16));
-            up = fmaxf(up, __shfl_xor(up, 32));
+            float up = max_over_rows(mx[c]);
             if (seen) up = fmaxf(up, 0.f);
             if (up == -INFINITY) up = 0.f;  // (the column sees none of these keys and has seen none before)
             else st.limit[c] = kLazyMax;
@@ -446,8 +445,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
     // ---- the key groups meet in LDS, then 16 rows of a wavefront are done ----
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-        st.l[c] += __shfl_xor(st.l[c], 16);
-        st.l[c] += __shfl_xor(st.l[c], 32);
+        st.l[c] = sum_over_rows(st.l[c]);
         if (st.limit[c] == -INFINITY) st.m[c] = -INFINITY;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) st.o[c][dt] += st.excess[c];
@@ -519,8 +517,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         for (int r = 0; r < 4; ++r) big = fmaxf(big, fabsf(st.o[0][dt][r]));
     const float inv = l == 0.f ? 0.f : 1.0f / l;  // (0: none of the split's keys is visible to the row)
     big *= inv;
-    big = fmaxf(big, __shfl_xor(big, 16));
-    big = fmaxf(big, __shfl_xor(big, 32));
+    big = max_over_rows(big);
     const int se = min(max(127 + 14 + 127 - (int)((__float_as_uint(big) >> 23) & 255u), 1), 254);
     const float scale = __uint_as_float((unsigned)se << 23);
     const int64_t pr = ((int64_t)split * p.Hkv + g) * p.M + row;
