@@ -10,7 +10,7 @@
 // instructions of the decode kernel take them, so that a wavefront moves a block from memory to the multiplier's registers with
 // ten loads of 16 bytes per lane and no exchange between lanes:
 //   K (A operand of 16 keys x 64 dims, lane = 16 h + key % 16, 16 bytes per lane): [key / 16][dims 64 ds ..][lane][16],
-//     bytes 0..7 of a lane: dims 64 ds + 8 h .., bytes 8..15: 64 ds + 32 + 8 h ..; two's complement
+//     bytes 0..7 of a lane: dims 64 ds + 8 h .., bytes 8..15: 64 ds + 32 + 8 h ..; code + 128
 //   V (A operand of 16 dims x 32 keys, lane = 16 h + dim / 8): [dim % 8][lane][8], two dims % 8 together in 16 bytes of a
 //     lane; bytes 4 kt + r of a lane: key 16 kt + 4 h + r, which is where the product of K leaves that key's score; code + 128
 //   scales: [key] (bf16 of K, bf16 of V)
@@ -94,12 +94,11 @@ __device__ __forceinline__ Divisor divisor_of(unsigned scale_bits) {
     d.r = fmaf(fmaf(-d.s, r, 1.0f), r, r);
     return d;
 }
-// The code of one of the two values in a word, in the low byte (two's complement, plus 128 for V).
-template <bool kPlus128>
+// The code of one of the two values in a word, plus 128, in the low byte.
 __device__ __forceinline__ unsigned code_of(unsigned pair, bool high, const Divisor& d) {
     const float x = __uint_as_float(high ? pair & 0xffff0000u : pair << 16) * d.up, t = x * d.r;
-    // (1.5 * 2^23 on top: the fraction goes, ties to even, and the whole number stands in the low bits)
-    return __float_as_uint(fmaf(fmaf(-t, d.s, x), d.r, t) + (kPlus128 ? 12583040.0f : 12582912.0f));
+    // (1.5 * 2^23 + 128 on top: the fraction goes, ties to even, and the whole number + 128 stands in the low bits)
+    return __float_as_uint(fmaf(fmaf(-t, d.s, x), d.r, t) + 12583040.0f);
 }
 // The low bytes of four words as one.
 __device__ __forceinline__ unsigned bytes_of(unsigned a, unsigned b, unsigned c, unsigned d) {
@@ -112,8 +111,8 @@ __device__ __forceinline__ unsigned quantise(const raw16& k, const raw16& v, uin
     unsigned w[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        w[j] = code_of<false>(k[j >> 1], j & 1, kd);
-        v_codes[j] = code_of<true>(v[j >> 1], j & 1, vd);
+        w[j] = code_of(k[j >> 1], j & 1, kd);
+        v_codes[j] = code_of(v[j >> 1], j & 1, vd);
     }
     k_codes = make_uint2(bytes_of(w[0], w[1], w[2], w[3]), bytes_of(w[4], w[5], w[6], w[7]));
     return ks | (vs << 16);
@@ -166,6 +165,15 @@ __device__ __forceinline__ void write_block(char* blk, const char* k, const char
         }
         *reinterpret_cast<raw16*>(blk + kBlockV + (dt >> 1) * 1024 + lane * 16) = w;
     }
+}
+
+// Stores and loads that pass the L2s, which are not coherent with one another.
+__device__ __forceinline__ void store_agent(void* dst, unsigned a, unsigned b) {
+    __hip_atomic_store(static_cast<unsigned long long*>(dst), (unsigned long long)a | ((unsigned long long)b << 32), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint2 load_agent(const void* src) {
+    const unsigned long long v = __hip_atomic_load(static_cast<const unsigned long long*>(src), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_uint2((unsigned)v, (unsigned)(v >> 32));
 }
 
 // K and V rows [n_caches][n_tokens][Hkv][128], their rows first_kept .. n_tokens - 1, quantised into the rows behind lens.v[i] of cache i

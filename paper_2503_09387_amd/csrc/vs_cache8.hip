@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kThreads) void cache8_read_kernel(RowsParams p) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const unsigned kw = j < 4 ? k[u].x : k[u].y;
-            kx[j] = (__bf16)((float)(int)(signed char)(kw >> (8 * (j & 3))) * ks);  // (15 + 8 bits: exact before the rounding)
+            kx[j] = (__bf16)((float)((int)((kw >> (8 * (j & 3))) & 255u) - 128) * ks);  // (15 + 8 bits: exact before the rounding)
             const unsigned vw = v[j >> 1][2 * (j & 1) + (u >> 2)];
             vx[j] = (__bf16)((float)((int)((vw >> (8 * (u & 3))) & 255u) - 128) * vs);
         }
@@ -246,7 +246,8 @@ vs_status vs_cache8_prefill_attn(const vs_shape* shape, vs_cache8* cache, const 
     const size_t ctrl = control_block_bytes(*shape);
     if (!workspace || workspace_bytes < ctrl + prefill8_workspace_need(*shape, n_tokens, len)) return VS_ERR_WORKSPACE;
     if (!aligned16(workspace)) return VS_ERR_ALIGN;
-    if (launch_prefill8(*shape, cache->data, len, q, k_t, v_t, n_tokens, first_kept, out, static_cast<char*>(workspace) + ctrl,
+    char* const ws = static_cast<char*>(workspace);
+    if (launch_prefill8(*shape, cache->data, len, q, k_t, v_t, n_tokens, first_kept, out, ws + ctrl,
                         static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return VS_ERR_HIP;
     cache->len += n_kept;

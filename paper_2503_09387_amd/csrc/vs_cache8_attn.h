@@ -38,7 +38,6 @@ __device__ __forceinline__ void widen(unsigned w, unsigned& lo, unsigned& hi) {
 
 // four codes of K as fp16, 1152 too large
 __device__ __forceinline__ void widen_key(unsigned w, unsigned& lo, unsigned& hi) {
-    w ^= 0x80808080u;
     lo = __builtin_amdgcn_perm(0x64646464u, w, 0x05010400u);
     hi = __builtin_amdgcn_perm(0x64646464u, w, 0x07030602u);
 }

@@ -130,15 +130,6 @@ __device__ __forceinline__ void put_row(Block& b, int key, uint2 k_codes, const 
     }
 }
 
-__device__ __forceinline__ void store_agent(float* dst, float a, float b) {
-    const unsigned long long v = (unsigned long long)__float_as_uint(a) | ((unsigned long long)__float_as_uint(b) << 32);
-    __hip_atomic_store(reinterpret_cast<unsigned long long*>(dst), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 load_agent(const float* src) {
-    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(src), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
-}
-
 // The shares of stream s, KV head g, added in index order: dims dp, dp + 1 of query head `head` of the group.  kAgent: the partial
 // results were stored in this launch, by other workgroups.
 template <bool kAgent>
@@ -152,8 +143,8 @@ __device__ __forceinline__ void add_shares(const Decode8Params& p, int s, int g,
 #pragma unroll
         for (int u = 0; u < kDepth; ++u) {
             const int64_t pr = pr0 + min(j0 + u, n_shares - 1) * step;
-            ml[u] = kAgent ? load_agent(p.part_ml + pr * 2) : *reinterpret_cast<const float2*>(p.part_ml + pr * 2);
-            o[u] = kAgent ? load_agent(p.part_o + pr * D + dp) : *reinterpret_cast<const float2*>(p.part_o + pr * D + dp);
+            ml[u] = kAgent ? __builtin_bit_cast(float2, load_agent(p.part_ml + pr * 2)) : *reinterpret_cast<const float2*>(p.part_ml + pr * 2);
+            o[u] = kAgent ? __builtin_bit_cast(float2, load_agent(p.part_o + pr * D + dp)) : *reinterpret_cast<const float2*>(p.part_o + pr * D + dp);
         }
         float mx = m;
 #pragma unroll
@@ -287,9 +278,9 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(Decode8Params p) {
             *reinterpret_cast<bf16x4*>(p.out + ((int64_t)s * p.Hq + (int64_t)g * p.G + head) * D + d) = r;
         } else {
             const int64_t pr = ((int64_t)share * p.Hkv + g) * p.G + head;
-            store_agent(p.part_o + pr * D + d, o[0], o[1]);
-            store_agent(p.part_o + pr * D + d + 2, o[2], o[3]);
-            if (d == 0) store_agent(p.part_ml + pr * 2, mx, l);
+            store_agent(p.part_o + pr * D + d, __float_as_uint(o[0]), __float_as_uint(o[1]));
+            store_agent(p.part_o + pr * D + d + 2, __float_as_uint(o[2]), __float_as_uint(o[3]));
+            if (d == 0) store_agent(p.part_ml + pr * 2, __float_as_uint(mx), __float_as_uint(l));
         }
     }
     if (n_shares == 1 || !p.counters) return;
