@@ -451,13 +451,13 @@ typedef struct {
     double turns[64]; /* revolutions of pair i per position: theta^(-i / n) / (2 pi); may be replaced, e.g. for stretched positions */
 } vs_rotary_plan;
 
-/* head_dim 64 or 128; sections of at least 0 whose sum is a multiple of 8, 8 .. head_dim / 2; theta > 0.  Host work only. */
+/* head_dim 64 or 128; sections of at least 0 whose sum is a multiple of 8, 8 .. head_dim / 2; theta > 0, its rates finite.  Host work only. */
 vs_status vs_rotary_plan_make(int32_t head_dim, const int32_t *sections, double theta, int32_t pairing, vs_rotary_plan *plan);
 
 /*
  * q, q_out [n_tokens][n_q_heads][head_dim], k, k_out [n_tokens][n_kv_heads][head_dim], positions int32 [3][n_tokens], all
  * device memory (positions 4-byte aligned).  q or k may be NULL, with its output.  An output may be its input (rows turned in place);
- * any other overlap of the two is refused (VS_ERR_SHAPE).  inverse != 0 turns back: the gradient of the rotation with
+ * any other overlap of an output with an input or with the other output is refused (VS_ERR_SHAPE).  inverse != 0 turns back: the gradient of the rotation with
  * respect to its input, and the way to give kept rows other positions.  1 <= n_tokens <= 2^26.  No workspace.
  */
 vs_status vs_rotary(const vs_shape *shape, const vs_rotary_plan *plan, const int32_t *positions, int32_t n_tokens, const void *q,
@@ -521,7 +521,7 @@ vs_status vs_cache8_decode_attn(const vs_shape *shape, int32_t n_streams, void *
  * are quantised into the cache and len grows by their number (n_tokens - 1: the carrier; 0: all, as vs_question_prefill_append;
  * n_tokens: none).  1 <= n_tokens <= 4096.  VS_ERR_CAPACITY, with nothing launched, if they do not fit; other errors
  * as vs_frame_prefill_attn, but for VS_ERR_PLACEMENT: no part of this call relies on where workgroups run.  A value of the run that is
- * not finite makes NaN of the outputs that it reaches, and of no others.
+ * not finite reaches the outputs of the tokens that see its row (of V, in its own dim), and no others.
  */
 vs_status vs_cache8_prefill_attn(const vs_shape *shape, vs_cache8 *cache, const void *q, const void *k_t, const void *v_t,
                                  int32_t n_tokens, int32_t first_kept, void *out, void *workspace, size_t workspace_bytes,

@@ -401,6 +401,7 @@ class RotaryPlan:
 
 def rotary(shape, plan, positions, q, k, q_out, k_out, inverse=False, stream=None):
     """positions: device int32 [3][T]; q, q_out [T][Hq][D], k, k_out [T][Hkv][D] (either pair may be None; in place: out is in)."""
+    assert positions.element_size() == 4 and positions.is_contiguous()
     _check(lib().vs_rotary(ctypes.byref(shape), ctypes.byref(plan.c), _ptr(positions), positions.shape[1], _ptr(q), _ptr(k), bool(inverse),
                            _ptr(q_out), _ptr(k_out), _stream(stream)), "vs_rotary")
 

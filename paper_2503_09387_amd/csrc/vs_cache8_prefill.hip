@@ -518,7 +518,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
     const float inv = l == 0.f ? 0.f : 1.0f / l;  // (0: none of the split's keys is visible to the row)
     big *= inv;
     big = max_over_rows(big);
-    const int se = min(max(127 + 14 + 127 - (int)((__float_as_uint(big) >> 23) & 255u), 1), 254);
+    const int se = min(max(127 + 14 + 127 - (int)((__float_as_uint(big) >> 23) & 255u), 1), 253);  // (2^126 at most: its inverse is a number too)
     const float scale = __uint_as_float((unsigned)se << 23);
     const int64_t pr = ((int64_t)split * p.Hkv + g) * p.M + row;
 #pragma unroll
@@ -578,6 +578,7 @@ __global__ __launch_bounds__(256) void prefill8_combine_kernel(Prefill8Params p)
 // Row tiles per workgroup, row groups, and workgroups that share a group's keys.
 struct Plan {
     int rt, groups, nsplit;
+    int most;  // splits that no run of as many tokens over fewer rows passes
 };
 Plan plan_of(const vs_shape& s, int32_t n_tokens, int32_t len) {
     const int G = s.n_q_heads / s.n_kv_heads, tiles = (n_tokens * G + kTileRows - 1) / kTileRows;
@@ -589,7 +590,7 @@ Plan plan_of(const vs_shape& s, int32_t n_tokens, int32_t len) {
     //   over 736 rows 27.9, 22.1 at 4, 23.1 at 6; over 4416 rows 85.7, 36.7 at 4, 32.5 at 6 (8, more than run at once: 46.0);
     //   37 tokens over 711 rows 23.8 at 1, 17.7 at 4, 16.7 at 12.
     const int blocks = (len + kBlockRows - 1) / kBlockRows + (n_tokens + 31) / 32, kg = kWaves / pl.rt, units = pl.groups * s.n_kv_heads;
-    pl.nsplit = std::max(1, std::min({256 / units, blocks / kg, kMaxSplits}));
+    pl.nsplit = pl.most = std::max(1, std::min({256 / units, blocks / kg, kMaxSplits}));
     if (pl.rt == 4 && blocks <= 13) pl.nsplit = 1;
     else if (pl.nsplit > 4 && units * pl.nsplit > 192 && blocks < 6 * pl.nsplit) pl.nsplit = std::max(4, blocks / 6);
     return pl;
@@ -602,10 +603,10 @@ size_t partial_bytes(const vs_shape& s, int32_t n_tokens, int nsplit) {
 
 size_t prefill8_workspace_need(const vs_shape& s, int32_t n_tokens, int32_t len) { return partial_bytes(s, n_tokens, plan_of(s, n_tokens, len).nsplit); }
 
-// What any run of at most max_tokens over at most max_len rows needs (splits come with more rows and go with more tokens).
+// What any run of at most max_tokens over at most max_len rows needs.
 size_t prefill8_workspace_bytes(const vs_shape& s, int32_t max_tokens, int32_t max_len) {
     size_t most = 0;
-    for (int32_t t = 1; t <= max_tokens; ++t) most = std::max(most, prefill8_workspace_need(s, t, max_len));
+    for (int32_t t = 1; t <= max_tokens; ++t) most = std::max(most, partial_bytes(s, t, plan_of(s, t, max_len).most));
     return most;
 }
 

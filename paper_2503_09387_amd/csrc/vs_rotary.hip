@@ -9,6 +9,8 @@
 // Bound by memory: every value is read once and written once.
 #include "vs_internal.h"
 
+#include <algorithm>
+
 #include <math.h>
 #include <string.h>
 
@@ -25,13 +27,14 @@ struct RotaryParams {
     char* k_out;
     const int32_t* pos;  // [3][n_tokens]
     int n_tokens, Hq, Hkv;
+    int first;           // token of the launch's first workgroup
     int pairs;           // rotated pairs of a head; the values behind them stay
     int ends[2];         // first pair of the second and of the third axis
     float sign;
     double turns[kMaxPairs];
 };
 
-// Grid: tokens.  The first wavefront works out the token's cosines and sines, a pair a lane, while every thread's values are on their
+// Grid: tokens, from p.first on.  The first wavefront works out the token's cosines and sines, a pair a lane, while every thread's values are on their
 // way.  A thread takes two pieces of 16 bytes of a head that hold whole pairs between them (so that a call may turn rows in place):
 // the same piece of both halves (pairs i, i + pairs), or 32 bytes in a row (pairs 2 i, 2 i + 1, and what is not turned).
 template <typename T, int D, bool kHalves>
@@ -39,7 +42,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p) {
     constexpr int N = 16 / (int)sizeof(T);
     constexpr int kUnits = D / (2 * N);  // of a head
     __shared__ float s_cos[kMaxPairs], s_sin[kMaxPairs];
-    const int t = blockIdx.x, tid = threadIdx.x, n_units = (p.Hq + p.Hkv) * kUnits;
+    const int t = p.first + blockIdx.x, tid = threadIdx.x, n_units = (p.Hq + p.Hkv) * kUnits;
     raw16 a, b;
     const T* src = nullptr;
     T* dst = nullptr;
@@ -97,18 +100,21 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p) {
 }
 
 template <typename T, int D>
-void launch(const RotaryParams& p, bool halves, hipStream_t st) {
-    if (halves) rotary_kernel<T, D, true><<<p.n_tokens, kThreads, 0, st>>>(p);
-    else rotary_kernel<T, D, false><<<p.n_tokens, kThreads, 0, st>>>(p);
+void launch(RotaryParams& p, bool halves, hipStream_t st) {
+    constexpr int kTokens = 1 << 20;  // of a launch, whose threads a grid counts in 32 bits
+    for (p.first = 0; p.first < p.n_tokens; p.first += kTokens) {
+        const int n = std::min(p.n_tokens - p.first, kTokens);
+        if (halves) rotary_kernel<T, D, true><<<n, kThreads, 0, st>>>(p);
+        else rotary_kernel<T, D, false><<<n, kThreads, 0, st>>>(p);
+    }
 }
 
 constexpr int32_t kMaxTokens = 1 << 26;
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-// the same memory, or none of it
-inline bool apart_or_same(const void* p, const void* q, int64_t bytes) {
+inline bool apart(const void* p, int64_t p_bytes, const void* q, int64_t q_bytes) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-    return a == b || a + (uintptr_t)bytes <= b || b + (uintptr_t)bytes <= a;
+    return a + (uintptr_t)p_bytes <= b || b + (uintptr_t)q_bytes <= a;
 }
 
 // pairs of a head that a plan turns, 0 if it is none
@@ -137,7 +143,10 @@ vs_status vs_rotary_plan_make(int32_t head_dim, const int32_t* sections, double 
     made.head_dim = head_dim;
     made.pairing = pairing;
     for (int i = 0; i < 3; ++i) made.sections[i] = sections[i];
-    for (int i = 0; i < n; ++i) made.turns[i] = pow(theta, -(double)i / n) / (2.0 * M_PI);
+    for (int i = 0; i < n; ++i) {
+        made.turns[i] = pow(theta, -(double)i / n) / (2.0 * M_PI);
+        if (!isfinite(made.turns[i])) return VS_ERR_SHAPE;
+    }
     *plan = made;
     return VS_OK;
 }
@@ -157,8 +166,9 @@ vs_status vs_rotary(const vs_shape* shape, const vs_rotary_plan* plan, const int
     RotaryParams p;
     p.Hq = q ? shape->n_q_heads : 0;
     p.Hkv = k ? shape->n_kv_heads : 0;
-    const int64_t head = (int64_t)n_tokens * shape->head_dim * (shape->dtype == VS_F32 ? 4 : 2);
-    if (!apart_or_same(q, q_out, p.Hq * head) || !apart_or_same(k, k_out, p.Hkv * head)) return VS_ERR_SHAPE;
+    const int64_t head = (int64_t)n_tokens * shape->head_dim * (shape->dtype == VS_F32 ? 4 : 2), nq = p.Hq * head, nk = p.Hkv * head;
+    if ((q != q_out && !apart(q, nq, q_out, nq)) || (k != k_out && !apart(k, nk, k_out, nk))) return VS_ERR_SHAPE;
+    if (q && k && (!apart(q_out, nq, k_out, nk) || !apart(q_out, nq, k, nk) || !apart(k_out, nk, q, nq))) return VS_ERR_SHAPE;
     p.q = (const char*)q;
     p.k = (const char*)k;
     p.q_out = (char*)q_out;

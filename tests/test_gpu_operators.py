@@ -94,6 +94,20 @@ def test_rotary(dtype, dim, sections, pairing, inverse, tokens, hq, hkv):
     assert same_bits(qi, qo)
 
 
+def test_rotary_of_more_tokens_than_a_launch_takes():
+    sh, T, sections = vs.Shape.make(1, 1, 64, "f32"), 2 ** 24 + 5, (8, 12, 12)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    k = torch.randn((T, 1, 64), generator=g, device=DEV)
+    pos = torch.randint(-100000, 100000, (3, T), generator=g, device=DEV, dtype=torch.int32)
+    out = torch.full_like(k, float("nan"))
+    vs.rotary(sh, vs.RotaryPlan(64, sections), pos, None, k, None, out)
+    some = [0, 1, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 1, 2 ** 24 - 1, 2 ** 24, T - 1]
+    where = pos[:, some].cpu().numpy()
+    want = ref.rotate(f64(k[some]), where, sections, 1e6, True)
+    assert (np.abs(f64(out[some]) - want) <= rotary_bound(f64(k[some]), want, where, torch.float32)).all()
+    assert torch.isfinite(out).all()
+
+
 def test_rotary_inverse_is_the_gradient():
     """The rotation is linear: <rot(x), y> = <x, inv(y)> for all x, y, and its differences are itself.  fp32: each of the two
     sums of n products is off by at most sum|x||y| 2^-20.5 (the rotation, see rotary_bound) in any order of 64-bit sums."""
@@ -315,6 +329,38 @@ def test_decode_peaked_and_flat_and_extreme():
         check_decode(sh, out, 0, qq, k, v, None, None, n, name)
 
 
+@pytest.mark.parametrize("fill", [0x00, 0xFF, 0x3C])
+def test_decode_with_a_workspace_that_was_not_prepared(fill):
+    """Arrival counters that hold anything: a stream's first share does the stream.  Then prepared again, and a workspace of other use."""
+    lens0 = [3000, 20, 700]
+    sh, slab, cap, lens, k, v, q, kn, vn = decode_case(28, 4, lens0, 600)
+    ws = torch.full((vs.cache8_workspace_bytes(sh, 0, cap, 3),), fill, dtype=torch.uint8, device=DEV)
+    was = slab.clone()
+    for turn in range(3):
+        if turn == 2:
+            vs.workspace_init(sh, ws)
+        slab.copy_(was)
+        lens = lens_array(lens0)
+        out = torch.full_like(q, float("nan"))
+        vs.cache8_decode_attn(sh, slab, cap, lens, q, kn, vn, out, ws)
+        for i, n0 in enumerate(lens0):
+            check_decode(sh, out, i, q, k, v, kn, vn, n0, f"turn {turn}, stream {i}")
+        expect = was.clone()
+        vs.cache8_append(sh, expect, cap, lens_array(lens0), kn[:, None].contiguous(), vn[:, None].contiguous())
+        assert same_bits(slab, expect)
+
+
+def test_decode_of_one_long_and_many_short_streams():
+    """Shares that a second launch adds (a stream of 64000 rows beside one of 1 row), and no new row."""
+    lens0 = [64000, 1]
+    sh, slab, cap, lens, k, v, q, kn, vn = decode_case(8, 2, lens0, 610, append=False)
+    ws = vs.make_cache8_workspace(sh, 0, cap, 2, DEV)
+    out = torch.full_like(q, float("nan"))
+    vs.cache8_decode_attn(sh, slab, cap, lens, q, None, None, out, ws)
+    for i, n0 in enumerate(lens0):
+        check_decode(sh, out, i, q, k, v, kn, vn, n0, f"stream {i}")
+
+
 # ---------------------------------------------------------------------------- prefill
 @pytest.mark.parametrize("hq,hkv", [(28, 4), (8, 1), (5, 5)])
 @pytest.mark.parametrize("L,T,kept", [(0, 1, 1), (0, 50, 50), (1, 1, 0), (31, 2, 2), (32, 170, 1), (33, 37, 37), (700, 37, 37), (711, 170, 1), (2000, 1, 1),
@@ -411,6 +457,45 @@ def test_prefill_extremes():
             bound = ref.decode_bound(f64(q1[t]), kk[:L + t + 1], vv[:L + t + 1], want[0], absolute[0], most[0], scale)
             err = np.abs(f64(out[t]) - want[0])
             assert np.isfinite(err).all() and (err <= bound).all(), f"{name}, token {t}: {(err / bound).max():.2f}"
+
+
+@pytest.mark.parametrize("L,T", [(900, 40), (900, 3)])
+def test_prefill_of_values_near_the_smallest(L, T):
+    """Values of 2^-114: what the splits of a row pass on is scaled up into fp16, and down again without loss."""
+    s = AttnShape(8, 2, 128, "bf16")
+    sh = vs_shape(s)
+    slab, lens = slab_of(sh, 1, L + T), lens_array([0])
+    k, kt, q = rows(95, 1, L, 2, 128), rows(96, T, 2, 128, loud=False), torch.zeros((T, 8, 128), dtype=torch.bfloat16, device=DEV)
+    v, vt = torch.full_like(k, 2.0 ** -114), torch.full_like(kt, -(2.0 ** -114))
+    vs.cache8_append(sh, slab, L + T, lens, k, v)
+    out = torch.full_like(q, float("nan"))
+    vs.cache8_prefill_attn(sh, vs.Cache8(slab[0], L + T, L), q, kt, vt, out, vs.make_cache8_workspace(sh, T, L, 0, DEV))
+    kk, vv = (np.concatenate([ref.stands_for(f64(a[0])), f64(b)]) for a, b in ((k, kt), (v, vt)))
+    for t in (0, T - 1):
+        want, absolute, most = ref.attend(f64(q[t:t + 1]), kk, vv, [L + t + 1], scale32(s))
+        bound = ref.decode_bound(f64(q[t]), kk[:L + t + 1], vv[:L + t + 1], want[0], absolute[0], most[0], scale32(s))
+        assert (np.abs(f64(out[t]) - want[0]) <= bound).all(), t
+
+
+def test_prefill_of_the_longest_run():
+    """4096 tokens over 50 rows, all kept: the rows kept fill planes of workgroups of their own."""
+    s = AttnShape(8, 2, 128, "bf16")
+    sh, L, T = vs_shape(s), 50, 4096
+    slab, lens = slab_of(sh, 1, L + T), lens_array([0])
+    k, v = rows(97, 1, L, 2, 128, loud=False), rows(98, 1, L, 2, 128, loud=False)
+    vs.cache8_append(sh, slab, L + T, lens, k, v)
+    q, kt, vt = rows(99, T, 8, 128, loud=False, sigma=2.0), rows(101, T, 2, 128, loud=False), rows(102, T, 2, 128, loud=False)
+    was, out = slab.clone(), torch.full_like(q, float("nan"))
+    cache = vs.Cache8(slab[0], L + T, L)
+    vs.cache8_prefill_attn(sh, cache, q, kt, vt, out, vs.make_cache8_workspace(sh, T, L, 0, DEV), first_kept=0)
+    assert cache.len == L + T
+    kk, vv = (np.concatenate([ref.stands_for(f64(a[0])), f64(b)]) for a, b in ((k, kt), (v, vt)))
+    tokens = [0, 31, 2047, 2048, 4095]
+    want, absolute, _ = ref.attend(f64(q)[tokens], kk, vv, [L + t + 1 for t in tokens], scale32(s))
+    check_close(out[tokens], want, "bf16", "longest run", absolute=False, abs_v_out=absolute)
+    assert torch.isfinite(out.float()).all()
+    vs.cache8_append(sh, was, L + T, lens, kt[None], vt[None])
+    assert same_bits(slab, was)
 
 
 # ---------------------------------------------------------------------------- as they are used together
@@ -512,6 +597,40 @@ def test_on_another_stream_and_captured():
     for turn in range(3):
         again(graph.replay)
         again(pass_)
+
+
+def test_two_graphs_over_one_workspace():
+    """A prefill and a decoding step in a graph each, replayed in turn with eager calls between, all over the same workspace."""
+    sh, slab, cap, _, k, v, q, kn, vn = decode_case(28, 4, [2500, 900], 700, cap=2600)
+    T = 37
+    qf, kf, vf = rows(701, T, 28, 128, loud=False), rows(702, T, 4, 128, loud=False), rows(703, T, 4, 128, loud=False)
+    ws = vs.make_cache8_workspace(sh, T, cap, 2, DEV)
+    of, od = torch.empty_like(qf), torch.empty_like(q)
+
+    def frame():
+        vs.cache8_prefill_attn(sh, vs.Cache8(slab[1], cap, 900), qf, kf, vf, of, ws, first_kept=T)
+
+    def step():
+        vs.cache8_decode_attn(sh, slab, cap, lens_array([2500, 900]), q, kn, vn, od, ws)
+
+    frame(), step()
+    torch.cuda.synchronize()
+    want = of.clone(), od.clone()
+    graphs = []
+    for call in (frame, step):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call()
+    for order in ((0, 1), (1, 0), (1, 1), (0, 0), (0, 1)):
+        of.fill_(float("nan")), od.fill_(float("nan"))
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for i, (got, first) in enumerate(zip((of, od), want)):
+            assert i not in order or same_bits(got, first)
+        step(), frame()
+        torch.cuda.synchronize()
+        assert same_bits(of, want[0]) and same_bits(od, want[1])
 
 
 def test_more_than_4_gib_of_rows():

@@ -115,6 +115,11 @@ def test_rotary_argument_errors():
     assert rot(shape=_shape(d=96)) == 3 and rot(shape=_shape(hq=28, hkv=5)) == 2
     assert rot(q=ODD) == 6 and rot(ko=ODD) == 6 and rot(pos=FAKE + 2) == 6
     assert rot(qo=FAKE + 256) == 2 and rot(ko=FAKE - 16) == 2        # overlaps its input without being it
+    # Q's output where K or its output lies, and the reverse: 4 tokens, 28 heads and 4 heads of 256 bytes
+    far = FAKE + (1 << 20)
+    assert rot(k=far, ko=FAKE) == 2 and rot(k=far, ko=FAKE + 4 * 28 * 256 - 16) == 2
+    assert rot(k=far, ko=far, qo=far + 4 * 4 * 256 - 16) == 2 and rot(k=far, ko=far, qo=far - 4 * 28 * 256 + 16) == 2
+    assert make(theta=5e-324) == 2                                   # rates beyond what fp64 holds
     broken = binding._CRotaryPlan.from_buffer_copy(plan)
     broken.sections[1] = 23
     assert rot(plan=broken) == 2
@@ -142,6 +147,18 @@ def test_cache8_sizes():
     for bad in ((-1, 0, 0), (4097, 0, 0), (1, -1, 0), (1, 0, -1), (1, 0, 1025)):
         assert vs.cache8_workspace_bytes(s, *bad) == 0
     assert vs.cache8_workspace_bytes(_shape(4, 1, 64, vs.VS_F32), 4, 4, 1) == 0
+
+
+@pytest.mark.parametrize("hq,hkv", [(28, 4), (24, 24), (8, 8), (8, 1), (5, 5)])
+def test_a_workspace_serves_any_run_over_fewer_rows(hq, hkv):
+    """The size is what the neediest run within the limits takes: it never falls as the limits go up."""
+    s = _shape(hq, hkv)
+    for tokens in (1, 9, 64, 107, 128, 300):
+        sizes = [vs.cache8_workspace_bytes(s, tokens, 32 * b, 0) for b in range(80)]
+        assert sizes == sorted(sizes), tokens
+    for rows in (0, 300, 1000, 3000):
+        sizes = [vs.cache8_workspace_bytes(s, t, rows, 0) for t in range(1, 400, 7)]
+        assert sizes == sorted(sizes), rows
 
 
 def test_cache8_append_and_read_argument_errors():
