@@ -1,11 +1,11 @@
 // Prefill attention over a cache in 8 bits (Eq. 1 of Section 3.1; Section 3.3): a run's tokens over the retained rows and, causally, over
-// one another.  The arithmetic is in vs_cache8_attn.h.  The G query heads of a KV head are packed into rows (row = token * G + head).  A wavefront holds 32 rows (two sets of 16 columns) and walks
-// blocks of 32 keys.  A workgroup is 8 wavefronts, kRT row tiles x 8 / kRT key groups, which are added in LDS at the end:
+// one another.  The arithmetic is in vs_cache8_attn.h.  The G query heads of a KV head are packed into rows (row = token * G + head).
+// A wavefront holds 32 rows (two sets of 16 columns) and walks blocks of 32 keys.  A workgroup is 8 wavefronts, kRT row tiles x 8 / kRT key groups, which are added in LDS at the end:
 //   * kRT = 4: two key groups, a wavefront of each on every SIMD.  A block comes from memory once, a quarter by each wavefront of
 //     its group, which widens its quarter into LDS for all four (widening costs as many vector instructions as the softmax of 32 rows).
 //     The groups take turns, a barrier apart: while one multiplies (the last block's values, the next one's keys), the other works out
 //     probabilities and widens, so that matrix and vector instructions of a SIMD run side by side.
-//   * kRT = 1, for up to 64 rows: every wavefront has a block of its own, straight from memory into the multiplier.
+//   * kRT = 1: every wavefront has a block of its own, straight from memory into the multiplier (which of the two: plan_of).
 #include "vs_cache8_attn.h"
 
 #include <algorithm>
@@ -27,8 +27,8 @@ struct Prefill8Params {
     const char* k;   // the run's own rows
     const char* v;
     __bf16* out;
-    _Float16* part_o;  // [split][Hkv][row] normalised, times the power of two that brings the row's largest entry into [2^14, 2^15)
-    float* part_ml;    // [split][Hkv][row][4]: reference (log2 units), sum, inverse of the row's scale, unused
+    _Float16* part_o;  // [split][Hkv][row][128] normalised, times the power of two that brings the largest of 32 dims into [2^14, 2^15)
+    char* part_ml;     // [split][Hkv][row][16 bytes]: reference (log2 units), sum, the biased exponents of the four powers, unused
     int len, T, G, Hq, Hkv, M;
     int n_cache_blocks;
     int n_groups;      // row groups: kRT * 32 rows each
@@ -224,6 +224,12 @@ __device__ __forceinline__ void attend_own(State& st, bf16x8 (&keys)[2][4], cons
     multiply_values<false>(st, p, [&](int dt) { return columns_of(x, dt); });
 }
 
+// The value of another lane of the same four (kSelect: two bits of each lane's source).
+template <int kSelect>
+__device__ __forceinline__ float neighbour(float x) {
+    return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kSelect, 0xf, 0xf, false));
+}
+
 // Grid (splits, Hkv, row groups and more): workgroups that read the same keys are Hkv * splits apart.  Those beyond the row groups quantise the
 // rows that are kept, a block and KV head each wavefront; whoever attends to the block they go to leaves out rows from len on.
 template <int kRT>
@@ -281,9 +287,9 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         for (int i = 0; i < 4; ++i) query[c][i] = *reinterpret_cast<const raw16*>(at + 64 * i);
         last[c] = t;
     }
-    // the run's own blocks
+    // the run's own blocks (kRT = 1: from the last key group on, the first ones have one more of the cache's if any)
     auto own_blocks = [&] {
-        int j = max(first, p.n_cache_blocks) + kg - p.n_cache_blocks;
+        int j = max(first, p.n_cache_blocks) + (kShared ? kg : kKG - 1 - kg) - p.n_cache_blocks;
         const int own_end = end - p.n_cache_blocks;
         if (j >= own_end) return;
         const char *const k = p.k + (int64_t)g * 256, *const v = p.v + (int64_t)g * 256;
@@ -472,6 +478,33 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) o[dt] = o[dt] * a + *reinterpret_cast<const f32x4*>(from + (dt * 64 + lane) * 4) * b2;
     };
+    // 8 values of a row, dims 32 hs + 8 r .. (hs: any quarter), times inv, to the output or, times 2^(se - 127), to the split's partial results
+    auto store = [&](int row, int hs, int r, const float (&o)[8], float inv, int se) {
+        if (row >= p.M) return;
+        if (p.nsplit == 1) {
+            const int t = token_of(row);
+            bf16x8 w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = (__bf16)(o[e] * inv);
+            *reinterpret_cast<bf16x8*>(p.out + ((int64_t)t * p.Hq + (int64_t)g * p.G + row - t * p.G) * D + 32 * hs + 8 * r) = w;
+        } else {
+            const float scale = __uint_as_float((unsigned)se << 23);
+            f16x8 w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = (_Float16)(o[e] * inv * scale);
+            *reinterpret_cast<f16x8*>(p.part_o + (((int64_t)split * p.Hkv + g) * p.M + row) * D + 32 * hs + 8 * r) = w;
+        }
+    };
+    auto store_sums = [&](int row, int hs, float m, float l, int se) {
+        if (row >= p.M || p.nsplit == 1) return;
+        char* const to = p.part_ml + (((int64_t)split * p.Hkv + g) * p.M + row) * 16;
+        to[8 + hs] = (char)se;
+        if (hs == 0) *reinterpret_cast<float2*>(to) = make_float2(m, l);
+    };
+    auto inverse_of = [&](float l) { return l == 0.f && p.nsplit > 1 ? 0.f : 1.0f / l; };  // (0: none of the split's keys is visible to the row)
+    auto exponent_of = [](float big) {  // (2^126 at most: its inverse is a number too)
+        return min(max(127 + 14 + 127 - (int)((__float_as_uint(big) >> 23) & 255u), 1), 253);
+    };
     if constexpr (kShared) {  // each group of two does one set of columns
         if (kg == 0) put(wave, st.o[1], st.m[1], st.l[1]);
         else put(wave, st.o[0], st.m[0], st.l[0]);
@@ -483,53 +516,53 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
             st.l[0] = st.l[1];
         }
         add(st.o[0], st.m[0], st.l[0], (wave + kRT) % kWaves);
-    } else {  // every wavefront leaves both; two of them add a set each, in the order of the groups
+        const int row = row0 + 16 * kg + i16;
+        float big = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) big = fmaxf(big, fabsf(st.o[0][dt][r]));
+        const float inv = inverse_of(st.l[0]);
+        const int se = exponent_of(big * inv);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = st.o[0][e][r];
+            store(row, h, r, o, inv, se);
+        }
+        store_sums(row, h, st.m[0], st.l[0], se);
+    } else {
+        // every wavefront leaves both, and adds 32 dims of one set in the order of the groups, a lane dims 8 (lane % 4) .. of column lane / 4 (two
+        // wavefronts with a set each: 1 us more)
         put(2 * wave, st.o[0], st.m[0], st.l[0]);
         put(2 * wave + 1, st.o[1], st.m[1], st.l[1]);
         __syncthreads();
-        if (wave >= 2) return;
-        st.m[0] = -INFINITY;
-        st.l[0] = 0.f;
+        const int set = wave & 1, quarter = wave >> 1, column = lane >> 2, row = row0 + 16 * set + column;
+        const float* const from = box + set * kBox;
+        float m[kWaves], l = 0.f, o[8] = {};
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) st.o[0][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-        for (int n = 0; n < kWaves; ++n) add(st.o[0], st.m[0], st.l[0], 2 * n + wave);
-    }
-    const int row = row0 + 16 * (kShared ? kg : wave) + i16;
-    const float l = st.l[0];
-    if (p.nsplit == 1) {
-        const float inv = 1.0f / l;
-        const int t = token_of(row);
-        __bf16* const dst = p.out + ((int64_t)t * p.Hq + (int64_t)g * p.G + row - t * p.G) * D + 32 * h;
+        for (int n = 0; n < kWaves; ++n) m[n] = from[2 * n * kBox + 2048 + column];
+        float mx = m[0];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            bf16x8 w;
+        for (int n = 1; n < kWaves; ++n) mx = fmaxf(mx, m[n]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = (__bf16)(st.o[0][e][r] * inv);
-            if (row < p.M) *reinterpret_cast<bf16x8*>(dst + 8 * r) = w;
+        for (int n = 0; n < kWaves; ++n) {
+            const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - mx);
+            l += f * from[2 * n * kBox + 2064 + column];
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) o[dt] += f * from[2 * n * kBox + dt * 256 + quarter * 64 + lane];
         }
-        return;
+        float big = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) big = fmaxf(big, fabsf(o[dt]));
+        big = fmaxf(big, neighbour<0xb1>(big));  // of the four lanes of a column
+        big = fmaxf(big, neighbour<0x4e>(big));
+        const float inv = inverse_of(l);
+        const int se = exponent_of(big * inv);
+        store(row, quarter, lane & 3, o, inv, se);
+        if ((lane & 3) == 0) store_sums(row, quarter, mx, l, se);
     }
-    float big = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) big = fmaxf(big, fabsf(st.o[0][dt][r]));
-    const float inv = l == 0.f ? 0.f : 1.0f / l;  // (0: none of the split's keys is visible to the row)
-    big *= inv;
-    big = max_over_rows(big);
-    const int se = min(max(127 + 14 + 127 - (int)((__float_as_uint(big) >> 23) & 255u), 1), 253);  // (2^126 at most: its inverse is a number too)
-    const float scale = __uint_as_float((unsigned)se << 23);
-    const int64_t pr = ((int64_t)split * p.Hkv + g) * p.M + row;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        f16x8 w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = (_Float16)(st.o[0][e][r] * inv * scale);
-        if (row < p.M) *reinterpret_cast<f16x8*>(p.part_o + pr * D + 32 * h + 8 * r) = w;
-    }
-    if (h == 0 && row < p.M)
-        *reinterpret_cast<float4*>(p.part_ml + pr * 4) = make_float4(st.m[0], l, __uint_as_float((unsigned)(254 - se) << 23), 0.f);
 }
 
 // The splits of a row added in index order: 16 lanes a row, 8 dims each.
@@ -542,12 +575,14 @@ __global__ __launch_bounds__(256) void prefill8_combine_kernel(Prefill8Params p)
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.f;
     for (int s0 = 0; s0 < p.nsplit; s0 += kDepth) {
-        float4 ml[kDepth];
+        float2 ml[kDepth];
+        unsigned se[kDepth];
         f16x8 x[kDepth];
 #pragma unroll
         for (int u = 0; u < kDepth; ++u) {
             const int64_t pr = ((int64_t)min(s0 + u, p.nsplit - 1) * p.Hkv + g) * p.M + row;
-            ml[u] = *reinterpret_cast<const float4*>(p.part_ml + pr * 4);
+            ml[u] = *reinterpret_cast<const float2*>(p.part_ml + pr * 16);
+            se[u] = *reinterpret_cast<const unsigned char*>(p.part_ml + pr * 16 + 8 + (d8 >> 5));
             x[u] = *reinterpret_cast<const f16x8*>(p.part_o + pr * D + d8);
         }
         float mx = m;
@@ -561,7 +596,7 @@ __global__ __launch_bounds__(256) void prefill8_combine_kernel(Prefill8Params p)
 #pragma unroll
         for (int u = 0; u < kDepth; ++u) {
             if (s0 + u >= p.nsplit) continue;
-            const float w = (mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - mx)) * ml[u].y, wo = w * ml[u].z;
+            const float w = (mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - mx)) * ml[u].y, wo = w * __uint_as_float((254 - se[u]) << 23);
             l += w;
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] += wo * (float)x[u][e];
@@ -582,21 +617,34 @@ struct Plan {
 };
 Plan plan_of(const vs_shape& s, int32_t n_tokens, int32_t len) {
     const int G = s.n_q_heads / s.n_kv_heads, tiles = (n_tokens * G + kTileRows - 1) / kTileRows;
-    Plan pl;
-    pl.rt = tiles <= 2 ? 1 : 4;
-    pl.groups = (tiles + pl.rt - 1) / pl.rt;
-    // One workgroup per compute unit, and a block for every key group at least.  us for attention and merge, 28/4 heads, by splits:
-    //   170 tokens over 200 rows (13 blocks) 19.8 at 1, 22.7 at 2, 20.7 at 4; over 352 rows 21.9 at 1, 20.4 at 4, 21.0 at 6;
-    //   over 736 rows 27.9, 22.1 at 4, 23.1 at 6; over 4416 rows 85.7, 36.7 at 4, 32.5 at 6 (8, more than run at once: 46.0);
-    //   37 tokens over 711 rows 23.8 at 1, 17.7 at 4, 16.7 at 12.
-    const int blocks = (len + kBlockRows - 1) / kBlockRows + (n_tokens + 31) / 32, kg = kWaves / pl.rt, units = pl.groups * s.n_kv_heads;
-    pl.nsplit = pl.most = std::max(1, std::min({256 / units, blocks / kg, kMaxSplits}));
-    if (pl.rt == 4 && blocks <= 13) pl.nsplit = 1;
-    else if (pl.nsplit > 4 && units * pl.nsplit > 192 && blocks < 6 * pl.nsplit) pl.nsplit = std::max(4, blocks / 6);
+    const int cached = (len + kBlockRows - 1) / kBlockRows, own = (n_tokens + 31) / 32;
+    Plan pl{};
+    pl.most = 1;
+    float least = INFINITY;
+    auto consider = [&](int rt, int groups, int nsplit, float us) {
+        if (us >= least) return;
+        least = us, pl.rt = rt, pl.groups = groups, pl.nsplit = nsplit;
+    };
+    auto way = [&](int rt, float group, float block, float own_block) {
+        const int groups = (tiles + rt - 1) / rt, units = groups * s.n_kv_heads;
+        const float blocks = cached + own_block * own;
+        const int n = std::max(1, std::min({256 / units, (cached + own) * rt / kWaves, kMaxSplits}));
+        consider(rt, groups, 1, 3.5f + ((units + 255) / 256) * (group + block * blocks));
+        if (n > 1) consider(rt, groups, n, 3.5f + group + block * blocks / n + 5.0f);
+        pl.most = std::max(pl.most, n);
+    };
+    // What a call takes, in us, from what was measured: a launch, what a workgroup takes besides its blocks, and each of its blocks, as often
+    // as workgroups follow one another on a compute unit; or as many splits as run at once, a block for every key group at least,
+    // and the launch that adds them.  One tile a workgroup has no merge where four have one; four spend fewer instructions on a block.
+    // Attention and merge, us, one tile / four, tokens x rows: 28/4 heads 10x200 8.1 / 12.3, 37x711 11.6 / 17.4, 64x1500 16.3 / 21.3,
+    // 100x8000 35.8 / 33.5, 170x352 10.8 / 20.4, 170x2400 22.0 / 26.7, 170x4416 32.3 / 32.3, 170x11016 67.4 / 50.9, 600x1000 44.0 / 45.1,
+    // 1024x0 45.2 / 41.8; 64/8 heads 300x300 27.4 / 24.3, 170x11016 130 / 110; 8/1 heads 170x11016 26.5 / 29.5.
+    way(1, 4.2f, 0.173f, 1.0f);
+    way(4, 10.2f, 0.525f, 1.5f);  // (causal: the longest of a group's rows count)
     return pl;
 }
 size_t partial_bytes(const vs_shape& s, int32_t n_tokens, int nsplit) {
-    return nsplit <= 1 ? 0 : (size_t)nsplit * n_tokens * s.n_q_heads * (D * sizeof(_Float16) + 4 * sizeof(float));
+    return nsplit <= 1 ? 0 : (size_t)nsplit * n_tokens * s.n_q_heads * (D * sizeof(_Float16) + 16);
 }
 
 }  // namespace
@@ -629,8 +677,8 @@ hipError_t launch_prefill8(const vs_shape& s, void* cache, int32_t len, const vo
     p.n_groups = pl.groups;
     p.nsplit = pl.nsplit;
     p.scale_log2e = s.softmax_scale * kLog2e;
-    p.part_ml = (float*)workspace;
-    p.part_o = (_Float16*)(p.part_ml + (int64_t)pl.nsplit * p.M * p.Hkv * 4);
+    p.part_ml = (char*)workspace;
+    p.part_o = (_Float16*)(p.part_ml + (int64_t)pl.nsplit * p.M * p.Hkv * 16);
     p.by_G = (unsigned)(0xffffffffu / p.G + 1u);  // exact for row * G < 2^32
     p.first_kept = first_kept;
     p.n_keeping = first_kept < n_tokens ? ((len + n_tokens - first_kept - 1) / kBlockRows - len / kBlockRows + 1) * p.Hkv : 0;
