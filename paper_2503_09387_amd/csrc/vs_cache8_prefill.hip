@@ -5,7 +5,9 @@
 //     its group, which widens its quarter into LDS for all four (widening costs as many vector instructions as the softmax of 32 rows).
 //     The groups take turns, a barrier apart: while one multiplies (the last block's values, the next one's keys), the other works out
 //     probabilities and widens, so that matrix and vector instructions of a SIMD run side by side.
-//   * kRT = 1: every wavefront has a block of its own, straight from memory into the multiplier (which of the two: plan_of).
+//   * kRT = 1: every wavefront has a block of its own, straight from memory into the multiplier, widened as it is multiplied; no merge launch for
+//     many sizes.  Bound by vector instructions (237 of a block's turn, beside 34 matrix instructions, two wavefronts a SIMD).
+//   Which of the two: plan_of.
 #include "vs_cache8_attn.h"
 
 #include <algorithm>
@@ -17,7 +19,9 @@ constexpr int D = 128;
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kTileRows = 32;  // rows of a wavefront
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLazyMax = 8.0f;  // scores may exceed the reference maximum by 2^8 before it is refreshed
+constexpr float kLazyMax = 8.0f;     // scores may exceed the reference maximum by 2^8 before it is refreshed
+constexpr float kMaxWeight = 15.0f;  // log2 of the largest weight that goes into an fp16
+constexpr float kLazyOwn = 20.0f;    // as kLazyMax for a run's own rows, behind cached ones whose weights have set the reference
 constexpr int kMaxSplits = 32;
 constexpr int kAhead = 5;       // pieces of a block that are on their way from LDS
 
@@ -41,9 +45,9 @@ struct Prefill8Params {
 
 struct State {
     f32x4 o[2][8];     // [columns][dim % 8]: element r of lane (column i16, h): dim 8 (4 h + r) + dim % 8
-    f32x4 excess[2];   // 128 times the sum of p s_v, negative
+    f32x4 excess[2];   // what is too much in them, negative
     float m[2], l[2];  // reference (log2 units; 0 until a key has been seen), this lane's share of the sum
-    float limit[2];    // how far scores may pass the reference before it is refreshed: -INFINITY until a key has been seen
+    float limit[2];    // what scores (kRT = 1: weights) may come to before the reference is refreshed, log2: -INFINITY until a key has been seen
 };
 
 // Scores less the reference become probabilities; the sums take them.
@@ -77,7 +81,7 @@ __device__ __forceinline__ void soften(State& st, float (&x)[2][8]) {
         }
 }
 
-// The three steps of a block of cached rows.  Scores of its keys (k_of(kt, i): 16 keys, 32 dims):
+// The steps of a block of cached rows.  Scores of its keys (k_of(kt, i): 16 keys, 32 dims):
 template <typename KOf>
 __device__ __forceinline__ void multiply_keys(f32x4 (&s)[2][2], const Queries (&q)[2], KOf k_of) {
 #pragma unroll
@@ -93,7 +97,7 @@ __device__ __forceinline__ void multiply_keys(f32x4 (&s)[2][2], const Queries (&
             for (int c = 0; c < 2; ++c) s[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[c].q[i], s[kt][c], 0, 0, 0);
         }
 }
-// probabilities times the scales of V, of the first `valid` rows:
+// probabilities times the scales of V, of the first `valid` rows (kRT = 4):
 template <typename Then>
 __device__ __forceinline__ void weigh(State& st, bf16x8 (&p)[2], const f32x4 (&s)[2][2], const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Queries (&q)[2],
                                       int valid, int h, Then then) {
@@ -121,21 +125,66 @@ __device__ __forceinline__ void weigh(State& st, bf16x8 (&p)[2], const f32x4 (&s
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)(x[c][e] * v[e]);
 }
-// and their product with the values (v_of(dt): dims % 8 = dt of 32 keys).
-template <bool kCodes, typename VOf>
-__device__ __forceinline__ void multiply_values(State& st, const bf16x8 (&p)[2], VOf v_of) {
-    if (kCodes) {
-        const unsigned minus128 = 0xc300c300u;
-        const bf16x8 off = __builtin_bit_cast(bf16x8, u32x4{minus128, minus128, minus128, minus128});
+// The same for kRT = 1, where every wavefront widens V for itself and it matters that a code becomes an fp16 in a third of the instructions
+// that a bf16 takes.  The weights w = p s_v unit are then fp16 too, 11 bits, and it is w that the reference holds in range: at most 2^15, the largest
+// 2^6 when it is set; what is below 2^-14 loses bits, 2^-25 a key at most, of what has a key of 2^6.  p is an fp32 of any size up to
+// 2^96 (rows of zeros, of the smallest scale, that a query likes best).  unit: see the kernel.
+__device__ __forceinline__ void weigh_for_fp16(State& st, f16x8 (&w)[2], const f32x4 (&s)[2][2], const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Queries (&q)[2],
+                                               int valid, int h) {
+    float x[2][8], v[8];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) st.excess[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(off, p[c], st.excess[c], 0, 0, 0);
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) x[c][4 * kt + r] = fmaf(s[kt][c][r], ks[kt][r] * q[c].f, -st.m[c]);
+            v[4 * kt + r] = vs[kt][r];
+        }
+    if (valid < kBlockRows) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (16 * (e >> 2) + 4 * h + (e & 3) >= valid) {
+                x[0][e] = x[1][e] = -INFINITY;
+                v[e] = 0.f;
+            }
+    }
+    // (log2 of the weights of these 8 keys is at most this; if that passes the limit they are looked at one by one)
+    const float top = fmaxf(__builtin_amdgcn_logf(max_of_8(v)), -80.f);
+    const float mx[2] = {max_of_8(x[0]) + top, max_of_8(x[1]) + top};
+    if (__any(mx[0] > st.limit[0] || mx[1] > st.limit[1])) {  // rare after the first block
+        asm volatile("s_nop 15\n\ts_nop 15");  // (as in soften)
+        float log_v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) log_v[e] = fmaxf(__builtin_amdgcn_logf(v[e]), -80.f) - 6.f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const bool seen = st.limit[c] != -INFINITY;
+            float z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = x[c][e] + log_v[e];
+            float up = max_over_rows(max_of_8(z));
+            if (seen) up = fmaxf(up, 0.f);
+            if (up == -INFINITY) up = 0.f;
+            else st.limit[c] = kMaxWeight;
+            // (in two steps: scales of V that are far apart take up past 126 and leave the sum a part of the whole all the same)
+            const float half = seen ? __builtin_amdgcn_exp2f(-0.5f * up) : 1.f, keep = half * half;
+            st.m[c] += up;
+            st.l[c] = st.l[c] * half * half;
+            scale_in_place(st.excess[c], keep);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) scale_in_place(st.o[c][dt], keep);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[c][e] -= up;
+        }
     }
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) {
-        const bf16x8 a = v_of(dt);
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) st.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[c], st.o[c][dt], 0, 0, 0);
-    }
+        for (int e = 0; e < 8; ++e) {
+            const float p = __builtin_amdgcn_exp2f(x[c][e]);
+            st.l[c] += p;
+            w[c][e] = (_Float16)(p * v[e]);
+        }
 }
 
 // The keys of a block of the run's own rows, keys 32 j .., as the products take them.
@@ -147,9 +196,9 @@ __device__ __forceinline__ void ask_own_keys(bf16x8 (&to)[2][4], const char* k, 
         for (int i = 0; i < 4; ++i) to[kt][i] = *reinterpret_cast<const bf16x8*>(row + 64 * i);
     }
 }
-// Such a block: column c sees keys up to `last[c]` of the run.  The keys of block j + step are asked for on the way.
+// Such a block: column c sees keys up to `last[c]` of the run; sums in units of 1 / unit.  The keys of block j + step are asked for on the way.
 __device__ __forceinline__ void attend_own(State& st, bf16x8 (&keys)[2][4], const char* k, const char* v, int64_t row_bytes, int j, int step, int T,
-                                           const raw16 (&q)[2][4], float f, const int (&last)[2], int i16, int h) {
+                                           const raw16 (&q)[2][4], float f, const int (&last)[2], float unit, int i16, int h) {
     raw16 x[8];  // 8 keys, of each dims 8 i16 ..
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -220,8 +269,13 @@ __device__ __forceinline__ void attend_own(State& st, bf16x8 (&keys)[2][4], cons
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)z[c][e];
-    multiply_values<false>(st, p, [&](int dt) { return columns_of(x, dt); });
+        for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)(z[c][e] * unit);
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+        const bf16x8 a = columns_of(x, dt);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) st.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[c], st.o[c][dt], 0, 0, 0);
+    }
 }
 
 // The value of another lane of the same four (kSelect: two bits of each lane's source).
@@ -287,6 +341,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         for (int i = 0; i < 4; ++i) query[c][i] = *reinterpret_cast<const raw16*>(at + 64 * i);
         last[c] = t;
     }
+    // kRT = 1: a power of two that weights carry (and the sums), so that p of rows of V that are very small or large throughout stays in the range of an fp32
+    float unit = 1.f;
     // the run's own blocks (kRT = 1: from the last key group on, the first ones have one more of the cache's if any)
     auto own_blocks = [&] {
         int j = max(first, p.n_cache_blocks) + (kShared ? kg : kKG - 1 - kg) - p.n_cache_blocks;
@@ -295,7 +351,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         const char *const k = p.k + (int64_t)g * 256, *const v = p.v + (int64_t)g * 256;
         bf16x8 keys[2][4];
         ask_own_keys(keys, k, row_bytes, j, p.T, i16, h);
-        for (; j < own_end; j += kKG) attend_own(st, keys, k, v, row_bytes, j, kKG, p.T, query, p.scale_log2e, last, i16, h);
+        for (; j < own_end; j += kKG) attend_own(st, keys, k, v, row_bytes, j, kKG, p.T, query, p.scale_log2e, last, kShared ? 1.f : unit, i16, h);
     };
     int b = first + kg;  // the block that this wavefront is at
     if constexpr (kShared) {
@@ -418,20 +474,31 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         auto ask_values = [&] {
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const raw16*>(blk + kBlockV + j * 1024 + lane * 16);
+        };
+        auto ask_scales = [&] {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) pairs[kt] = *reinterpret_cast<const raw16*>(blk + kBlockScales + 64 * kt + 16 * h);
         };
         Queries q[2];
         if (b < stop) {
+            ask_scales();
             ask_keys();
             ask_values();
             q[0] = queries_of(query[0], p.scale_log2e);
             q[1] = queries_of(query[1], p.scale_log2e);
+            unsigned top = 0;  // the largest scale of V in the wavefront's first block (as a bit pattern, K's below it)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = max(top, 16 * kt + 4 * h + r < p.len - b * kBlockRows ? pairs[kt][r] : 0u);
+            top = __builtin_amdgcn_readfirstlane(over_rows(top, [](unsigned x, unsigned y) { return max(x, y); }));
+            if (top < __float_as_uint(0x1p-60f) && top >= __float_as_uint(0x1p-125f)) unit = 0x1p40f;  // (2^-126: rows of zeros)
+            else if (top > __float_as_uint(0x1p60f) && top < 0x7f800000u) unit = 0x1p-40f;
         }
         for (; b < stop; b += kKG) {
             if (b + kKG < stop) blk += kKG * stride;  // (behind the last one: that one again)
             f32x4 s[2][2], ks[2], vs[2];
-            bf16x8 weights[2];
+            f16x8 weights[2];
             multiply_keys(s, q, [&](int kt, int i) { return keys_of(k[2 * kt + (i >> 1)][2 * (i & 1)], k[2 * kt + (i >> 1)][2 * (i & 1) + 1]); });
             ask_keys();
 #pragma unroll
@@ -439,12 +506,25 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     ks[kt][r] = __uint_as_float(pairs[kt][r] << 16);
-                    vs[kt][r] = __uint_as_float(pairs[kt][r] & 0xffff0000u);
+                    vs[kt][r] = __uint_as_float(pairs[kt][r] & 0xffff0000u) * unit;
                 }
-            weigh(st, weights, s, ks, vs, q, p.len - b * kBlockRows, h, [] {});
-            multiply_values<true>(st, weights, [&](int dt) { return values_of(v[dt >> 1][2 * (dt & 1)], v[dt >> 1][2 * (dt & 1) + 1]); });
+            weigh_for_fp16(st, weights, s, ks, vs, q, p.len - b * kBlockRows, h);
+            const unsigned minus1152 = 0xe480e480u;
+            const f16x8 off = __builtin_bit_cast(f16x8, u32x4{minus1152, minus1152, minus1152, minus1152});
+#pragma unroll
+            for (int c = 0; c < 2; ++c) st.excess[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, weights[c], st.excess[c], 0, 0, 0);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) {
+                const f16x8 a = keys_of(v[dt >> 1][2 * (dt & 1)], v[dt >> 1][2 * (dt & 1) + 1]);  // (code + 1152, as K's)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) st.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, weights[c], st.o[c][dt], 0, 0, 0);
+            }
             ask_values();
+            ask_scales();
         }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            if (st.limit[c] != -INFINITY) st.limit[c] = kLazyOwn;
         own_blocks();
     }
 
@@ -455,6 +535,13 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         if (st.limit[c] == -INFINITY) st.m[c] = -INFINITY;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) st.o[c][dt] += st.excess[c];
+    }
+    if (!kShared && unit != 1.f) {
+        const float back = unit > 1.f ? 0x1p-40f : 0x1p40f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) st.o[c][dt] *= back;
     }
     __syncthreads();  // (blocks may still be read there)
     float* const box = reinterpret_cast<float*>(smem);
@@ -548,8 +635,9 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         for (int n = 1; n < kWaves; ++n) mx = fmaxf(mx, m[n]);
 #pragma unroll
         for (int n = 0; n < kWaves; ++n) {
-            const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - mx);
-            l += f * from[2 * n * kBox + 2064 + column];
+            // (the sum in two steps, as in weigh_for_fp16)
+            const float half = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (m[n] - mx)), f = half * half;
+            l += half * from[2 * n * kBox + 2064 + column] * half;
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) o[dt] += f * from[2 * n * kBox + dt * 256 + quarter * 64 + lane];
         }
@@ -588,15 +676,16 @@ __global__ __launch_bounds__(256) void prefill8_combine_kernel(Prefill8Params p)
         float mx = m;
 #pragma unroll
         for (int u = 0; u < kDepth; ++u) mx = fmaxf(mx, ml[u].x);
-        const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx);
-        l *= f;
+        const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (m - mx));
+        l = l * f * f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] *= f;
+        for (int e = 0; e < 8; ++e) o[e] = o[e] * f * f;
         m = mx;
 #pragma unroll
         for (int u = 0; u < kDepth; ++u) {
             if (s0 + u >= p.nsplit) continue;
-            const float w = (mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - mx)) * ml[u].y, wo = w * __uint_as_float((254 - se[u]) << 23);
+            // (in two steps, as in weigh_for_fp16)
+            const float half = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (ml[u].x - mx)), w = half * ml[u].y * half, wo = w * __uint_as_float((254 - se[u]) << 23);
             l += w;
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] += wo * (float)x[u][e];
@@ -636,11 +725,11 @@ Plan plan_of(const vs_shape& s, int32_t n_tokens, int32_t len) {
     // What a call takes, in us, from what was measured: a launch, what a workgroup takes besides its blocks, and each of its blocks, as often
     // as workgroups follow one another on a compute unit; or as many splits as run at once, a block for every key group at least,
     // and the launch that adds them.  One tile a workgroup has no merge where four have one; four spend fewer instructions on a block.
-    // Attention and merge, us, one tile / four, tokens x rows: 28/4 heads 10x200 8.1 / 12.3, 37x711 11.6 / 17.4, 64x1500 16.3 / 21.3,
-    // 100x8000 35.8 / 33.5, 170x352 10.8 / 20.4, 170x2400 22.0 / 26.7, 170x4416 32.3 / 32.3, 170x11016 67.4 / 50.9, 600x1000 44.0 / 45.1,
-    // 1024x0 45.2 / 41.8; 64/8 heads 300x300 27.4 / 24.3, 170x11016 130 / 110; 8/1 heads 170x11016 26.5 / 29.5.
-    way(1, 4.2f, 0.173f, 1.0f);
-    way(4, 10.2f, 0.525f, 1.5f);  // (causal: the longest of a group's rows count)
+    // Attention and merge, us, one tile / four, tokens x rows: 28/4 heads 10x200 8.5 / 12.4, 37x711 11.7 / 18.0, 64x1500 16.1 / 21.0,
+    // 100x8000 32.8 / 33.3, 170x352 11.0 / 20.4, 170x2400 20.4 / 26.2, 170x4416 29.1 / 32.1, 170x7000 40.5 / 39.4, 170x11016 58.0 / 50.5,
+    // 600x1000 42.7 / 45.6, 1024x0 45.5 / 41.8; 64/8 heads 300x300 28.8 / 24.6, 2048x200 269 / 227; 8/1 heads 170x11016 24.8 / 29.4.
+    way(1, 5.1f, 0.144f, 1.0f);
+    way(4, 10.2f, 0.525f, 1.25f);  // (causal: the longest of a group's rows count)
     return pl;
 }
 size_t partial_bytes(const vs_shape& s, int32_t n_tokens, int nsplit) {

@@ -55,6 +55,20 @@ def decode_bound(q, k, v, ref, absolute, most, scale):
     return 2.0 ** -8 * np.abs(ref) + 2.0 ** -8 * 1.01 * absolute + weights + 2.0 ** -24 * steps * 8.1 * most + 2.0 ** -126 * np.repeat(np.abs(v).sum(0), g, 0)
 
 
+def prefill_bound(q, k, v, ref, absolute, most, scale):
+    """The same for a token of a prefill, q [Hq][D], k and v its rows: on top of decode_bound
+    * partial results of splits are fp16, scaled so that the largest of 32 dims is in [2^14, 2^15): 2^-11 of a value, or 2^-25 where it is under
+      2^-14, 2^-39 of the largest; weighted by the splits' shares, 2^-11 of the terms' magnitudes and 2^-39 of the rows' largest;
+    * weights in fp16 instead of bf16: 2^-11 of a term (decode_bound has 2^-8), but 2^-25 under 2^-14, where the largest weight is at least 2^6
+      when the reference is set and the reference only goes up: 2^-31 of a row of its size, for each key;
+    * their sums go up to 1279 and back by 1152 a unit of weight, where a row's largest code is 126 at least: a rounding of 2^-24 of 2431 / 126 = 19.3
+      instead of 8.1 of the rows' largest, per 32 keys;
+    * a product of a probability and a scale of V that is under 2^-126 may be 0, beside a sum of at least 1: 2^-126 of a key's whole number, which is
+      at most 127 (decode_bound has 2^-126 of the value, which for scales under 1 is less)."""
+    n = k.shape[0]
+    return decode_bound(q, k, v, ref, absolute, most, scale) + 2.0 ** -11 * 1.01 * absolute + (2.0 ** -39 + 2.0 ** -31 * n + 2.0 ** -24 * (n // 32 + 8) * 11.2) * most + 2.0 ** -126 * 127 * n
+
+
 def rotate(x, positions, sections, theta, halves, inverse=False):
     """x [T][H][D] fp64, positions [3][T]."""
     n = sum(sections)

@@ -477,6 +477,37 @@ def test_prefill_of_values_near_the_smallest(L, T):
         assert (np.abs(f64(out[t]) - want[0]) <= bound).all(), t
 
 
+@pytest.mark.parametrize("hq,hkv,L,T", [(8, 2, 300, 40), (8, 2, 1000, 3), (28, 4, 300, 400), (28, 4, 300, 1000), (28, 4, 9000, 170)])
+def test_prefill_of_rows_of_very_different_sizes(hq, hkv, L, T):
+    """V in rows of zeros that a query likes best, first or throughout, of sizes 2^-40 .. 2^40, very large or very small first rows."""
+    s = AttnShape(hq, hkv, 128, "bf16")
+    sh = vs_shape(s)
+    k, v = rows(110, 1, L, hkv, 128), rows(111, 1, L, hkv, 128)
+    q, kt, vt = rows(112, T, hq, 128, loud=False, sigma=1.0), rows(113, T, hkv, 128, loud=False), rows(114, T, hkv, 128, loud=False)
+    like = (q.float().reshape(T, hkv, hq // hkv, 128).mean((0, 2)) * 300).to(torch.bfloat16)     # [Hkv][128]
+    size = torch.exp2(torch.randint(-40, 41, (1, L, hkv, 1), generator=torch.Generator(device=DEV).manual_seed(5), device=DEV).float())
+    row = torch.arange(L, device=DEV)[None, :, None, None]
+    first = row < 40
+    sink = torch.where(first, like[None, None], k)
+    cases = {"first rows of zeros": (k, torch.where(first, 0.0, v)), "first rows of zeros liked best": (sink, torch.where(first, 0.0, v)),
+             "all zeros": (k, v * 0), "many sizes": (k, v * size), "first rows large": (k, torch.where(first, v * 2.0 ** 100, v)),
+             "first rows tiny": (k, torch.where(first, v * 2.0 ** -100, v)), "a tiny row liked best": (torch.where(row == 37, like[None, None], k), torch.where(row == 37, v * 2.0 ** -90, v)),
+             "last rows large": (k, torch.where(row >= L - 20, v * 2.0 ** 60, v))}
+    ws = vs.make_cache8_workspace(sh, T, L, 0, DEV)
+    for name, (k1, v1) in cases.items():
+        k1, v1 = k1.to(torch.bfloat16), v1.to(torch.bfloat16)
+        slab, lens = slab_of(sh, 1, L + T), lens_array([0])
+        vs.cache8_append(sh, slab, L + T, lens, k1, v1)
+        out = torch.full_like(q, float("nan"))
+        vs.cache8_prefill_attn(sh, vs.Cache8(slab[0], L + T, L), q, kt, vt, out, ws)
+        kk, vv = (np.concatenate([ref.stands_for(f64(a[0])), f64(b)]) for a, b in ((k1, kt), (v1, vt)))
+        for t in sorted({0, T // 2, T - 1}):
+            want, absolute, most = ref.attend(f64(q[t:t + 1]), kk, vv, [L + t + 1], scale32(s))
+            bound = ref.prefill_bound(f64(q[t]), kk[:L + t + 1], vv[:L + t + 1], want[0], absolute[0], most[0], scale32(s))
+            err = np.abs(f64(out[t]) - want[0])
+            assert np.isfinite(err).all() and (err <= bound).all(), f"{name}, token {t}: {(err / bound).max():.2f}"
+
+
 def test_prefill_of_the_longest_run():
     """4096 tokens over 50 rows, all kept: the rows kept fill planes of workgroups of their own."""
     s = AttnShape(8, 2, 128, "bf16")
