@@ -6,7 +6,9 @@
 // A product of a position and a rate is taken in fp64 and only what is left of a whole revolution goes on in fp32: positions of a long
 // stream pass 10^5, and an angle of so many radians in fp32 is off by 10^-2.
 //
-// Bound by memory: every value is read once and written once.
+// Bound by memory: every value is read once and written once.  16384 tokens of 28/4 heads of 128 (269 MB) 40.4 us on the device, 48.2 us a call over
+// changing rows = 5.6 TB/s; 3200 tokens of 4/1 heads of 64 in fp32 4.6 us; 16 tokens 3.0 us, which is the launch and the trips to the
+// positions and the rows.
 #include "vs_internal.h"
 
 #include <algorithm>
