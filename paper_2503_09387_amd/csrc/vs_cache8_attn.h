@@ -7,8 +7,8 @@
 //     the query is an fp16 after the power of two that brings its largest entry into [2^14, 2^15), which loses nothing down to 2^-28
 //     of that entry and 2^-39 of it below; the sums start at -1152 sum q.
 //   * p s_v in bf16 (8 bits, as P does over caches in bf16; the denominator sums p before that) times the codes + 128 in bf16, which
-//     loses nothing, less 128 times the sum of p s_v, through one more product, with a matrix of -128.  (The prefill with a row tile a
-//     workgroup takes both as fp16: weigh_for_fp16.)
+//     loses nothing, less 128 times the sum of p s_v, through one more product, with a matrix of -128.  (The prefill
+//     takes both as fp16: see its `weigh`.)
 #pragma once
 #include "vs_cache8.h"
 

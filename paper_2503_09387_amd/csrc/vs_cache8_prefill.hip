@@ -1,15 +1,13 @@
 // Prefill attention over a cache in 8 bits (Eq. 1 of Section 3.1; Section 3.3): a run's tokens over the retained rows and, causally, over
 // one another.  The arithmetic is in vs_cache8_attn.h.  The G query heads of a KV head are packed into rows (row = token * G + head).
-// A wavefront holds 32 rows (two sets of 16 columns) and walks blocks of 32 keys.  A workgroup is 8 wavefronts, kRT row tiles x 8 / kRT key groups, which are added in LDS at the end:
-//   * kRT = 4: two key groups, a wavefront of each on every SIMD.  A block comes from memory once, a quarter by each wavefront of
-//     its group, which widens its quarter into LDS for all four (widening costs as many vector instructions as the softmax of 32 rows).
-//     The groups take turns, a barrier apart: while one multiplies (the last block's values, the next one's keys), the other works out
-//     probabilities and widens, so that matrix and vector instructions of a SIMD run side by side.
-//   * kRT = 1: every wavefront has a block of its own, straight from memory into the multiplier, widened as it is multiplied; no merge launch for
-//     many sizes.  Bound by vector instructions (237 of a block's turn, beside 34 matrix instructions, two wavefronts a SIMD).
-//   Which of the two: plan_of.
-// 28/4 heads: 37 tokens over 711 rows 11.4 us, 170 over 4424 30.3 us = 363 TFLOP/s (kRT = 1); 170 over 11016 49.6 us = 545 TFLOP/s, and 4.8 (kRT = 4).
-// Some 8 us of each are fixed: launch, first trips to memory, the queries' conversion, the sums' way through LDS, stores.
+// A wavefront holds 32 rows (two sets of 16 columns) and walks blocks of 32 keys, from memory into the multiplier, widened as they are multiplied.
+// A workgroup is 4 wavefronts that take the blocks of the same rows in turn and add their sums in LDS; two workgroups fit a compute unit, so
+// that one multiplies while the other starts or ends.  us by workgroup, 28/4 heads, 37 tokens over 711 rows, 170 over 11016, 600 over 1000, 2048 over 200:
+//   4 wavefronts 10.4, 47.4, 31.8, 95;  8, one workgroup to a compute unit 11.8, 58.2, 43.2, 125;  2 12.4, 48.8, 35.2, 97;
+//   8 of 128 rows that share a block, widened once, through LDS 17.4, 51.2, 45.8, 128.
+// Bound by vector instructions (some 200 of a block's turn, beside 34 matrix instructions, two wavefronts a SIMD; 170 over 11016 in three splits is
+// 650 TFLOP/s) and, for few blocks, by some 7 us of start and end: launch, first trips to memory, the queries' conversion, the sums' way
+// through LDS, stores.
 #include "vs_cache8_attn.h"
 
 #include <algorithm>
@@ -18,14 +16,13 @@ namespace vs {
 namespace {
 
 constexpr int D = 128;
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kTileRows = 32;  // rows of a wavefront
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kTileRows = 32;  // rows of a workgroup
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazyMax = 8.0f;     // scores may exceed the reference maximum by 2^8 before it is refreshed
 constexpr float kMaxWeight = 15.0f;  // log2 of the largest weight that goes into an fp16
 constexpr float kLazyOwn = 20.0f;    // as kLazyMax for a run's own rows, behind cached ones whose weights have set the reference
 constexpr int kMaxSplits = 32;
-constexpr int kAhead = 5;       // pieces of a block that are on their way from LDS
 
 struct Prefill8Params {
     char* cache;
@@ -37,7 +34,7 @@ struct Prefill8Params {
     char* part_ml;     // [split][Hkv][row][16 bytes]: reference (log2 units), sum, the biased exponents of the four powers, unused
     int len, T, G, Hq, Hkv, M;
     int n_cache_blocks;
-    int n_groups;      // row groups: kRT * 32 rows each
+    int n_tiles;       // of kTileRows rows
     int nsplit;
     int first_kept;    // rows of the run from this one on are kept,
     int n_keeping;     // (block, KV head) pairs that they fall into
@@ -49,7 +46,7 @@ struct State {
     f32x4 o[2][8];     // [columns][dim % 8]: element r of lane (column i16, h): dim 8 (4 h + r) + dim % 8
     f32x4 excess[2];   // what is too much in them, negative
     float m[2], l[2];  // reference (log2 units; 0 until a key has been seen), this lane's share of the sum
-    float limit[2];    // what scores (kRT = 1: weights) may come to before the reference is refreshed, log2: -INFINITY until a key has been seen
+    float limit[2];    // what weights, of a run's own rows scores, may come to before the reference is refreshed, log2: -INFINITY until a key has been seen
 };
 
 // Scores less the reference become probabilities; the sums take them.
@@ -99,39 +96,11 @@ __device__ __forceinline__ void multiply_keys(f32x4 (&s)[2][2], const Queries (&
             for (int c = 0; c < 2; ++c) s[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[c].q[i], s[kt][c], 0, 0, 0);
         }
 }
-// probabilities times the scales of V, of the first `valid` rows (kRT = 4):
-template <typename Then>
-__device__ __forceinline__ void weigh(State& st, bf16x8 (&p)[2], const f32x4 (&s)[2][2], const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Queries (&q)[2],
-                                      int valid, int h, Then then) {
-    float x[2][8], v[8];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c) x[c][4 * kt + r] = fmaf(s[kt][c][r], ks[kt][r] * q[c].f, -st.m[c]);
-            v[4 * kt + r] = vs[kt][r];
-        }
-    if (valid < kBlockRows) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (16 * (e >> 2) + 4 * h + (e & 3) >= valid) {
-                x[0][e] = x[1][e] = -INFINITY;
-                v[e] = 0.f;
-            }
-    }
-    soften(st, x);
-    then();
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)(x[c][e] * v[e]);
-}
-// The same for kRT = 1, where every wavefront widens V for itself and it matters that a code becomes an fp16 in a third of the instructions
-// that a bf16 takes.  The weights w = p s_v unit are then fp16 too, 11 bits, and it is w that the reference holds in range: at most 2^15, the largest
-// 2^6 when it is set; what is below 2^-14 loses bits, 2^-25 a key at most, of what has a key of 2^6.  p is an fp32 of any size up to
-// 2^96 (rows of zeros, of the smallest scale, that a query likes best).  unit: see the kernel.
-__device__ __forceinline__ void weigh_for_fp16(State& st, f16x8 (&w)[2], const f32x4 (&s)[2][2], const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Queries (&q)[2],
+// weights w = p s_v unit of the first `valid` rows, as fp16 like the codes of V: a code becomes an fp16 in a third of the instructions that a bf16
+// takes, and a weight has 11 bits.  It is w that the reference holds in range: at most 2^15, the largest 2^6 when it is set; what is below 2^-14 loses
+// bits, 2^-25 a key at most, of what has a key of 2^6.  p is an fp32 of any size up to 2^96 (rows of zeros, of the smallest scale, that a
+// query likes best).  unit: see the kernel.
+__device__ __forceinline__ void weigh(State& st, f16x8 (&w)[2], const f32x4 (&s)[2][2], const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Queries (&q)[2],
                                                int valid, int h) {
     float x[2][8], v[8];
 #pragma unroll
@@ -286,33 +255,27 @@ __device__ __forceinline__ float neighbour(float x) {
     return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kSelect, 0xf, 0xf, false));
 }
 
-// Grid (splits, Hkv, row groups and more): workgroups that read the same keys are Hkv * splits apart.  Those beyond the row groups quantise the
+// Grid (splits, Hkv, row tiles and more): workgroups that read the same keys are Hkv * splits apart.  Those beyond the tiles quantise the
 // rows that are kept, a block and KV head each wavefront; whoever attends to the block they go to leaves out rows from len on.
-template <int kRT>
 __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p) {
-    constexpr int kKG = kWaves / kRT;
-    constexpr bool kShared = kRT > 1;
-    static_assert(!kShared || kKG == 2, "two key groups take turns");
-    constexpr int kStaged = 16384 + 256;  // a widened block: K, V, the scales of K, the scales of V
-    constexpr int kLds = 16 * (8 * 64 * 4 + 32) * 4;  // both sets of columns of 8 wavefronts
-    __shared__ __attribute__((aligned(16))) char smem[kLds];
-    static_assert(3 * 2 * kStaged <= kLds, "three blocks of either key group: one each that values, keys and widening are at");
+    // a set of columns of a wavefront: [dim % 8][lane][r], then references and sums
+    constexpr int kBox = 8 * 64 * 4 + 32;
+    __shared__ __attribute__((aligned(16))) float box[2 * kWaves * kBox];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i16 = lane & 15, h = lane >> 4;
-    const int split = blockIdx.x, g = blockIdx.y, group = blockIdx.z;
+    const int split = blockIdx.x, g = blockIdx.y, tile = blockIdx.z;
     auto token_of = [&](int row) { return p.G == 1 ? row : (int)__umulhi((unsigned)row, p.by_G); };
-    if (group >= p.n_groups) {
-        const int item = (((group - p.n_groups) * p.Hkv + g) * p.nsplit + split) * kWaves + wave;
+    if (tile >= p.n_tiles) {
+        const int item = (((tile - p.n_tiles) * p.Hkv + g) * p.nsplit + split) * kWaves + wave;
         if (item >= p.n_keeping) return;
         const int kept = p.T - p.first_kept, block = p.len / kBlockRows + item / p.Hkv, head = item % p.Hkv;
         const int64_t row_bytes = (int64_t)p.Hkv * 256, src = p.first_kept * row_bytes + head * 256 + 16 * i16;
         write_block(p.cache + ((int64_t)block * p.Hkv + head) * kBlockBytes, p.k + src, p.v + src, row_bytes, block * kBlockRows, p.len, p.len + kept, lane);
         return;
     }
-    const int rt = wave % kRT, kg = wave / kRT;
-    const int row0 = (group * kRT + rt) * kTileRows;
-    // blocks that rows of the group see: the cache's and the run's own up to its last token
-    const int last_row = min((group + 1) * kRT * kTileRows, p.M) - 1;
+    const int row0 = tile * kTileRows;
+    // blocks that rows of the tile see: the cache's and the run's own up to its last token
+    const int last_row = min(row0 + kTileRows, p.M) - 1;
     // (an own block takes about twice a cached one's time: the shares are even in that measure)
     const unsigned total = p.n_cache_blocks + 2 * (token_of(last_row) / 32 + 1), share = total / p.nsplit, more = total - share * p.nsplit;
     auto border = [&](int s) {
@@ -343,230 +306,100 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         for (int i = 0; i < 4; ++i) query[c][i] = *reinterpret_cast<const raw16*>(at + 64 * i);
         last[c] = t;
     }
-    // kRT = 1: a power of two that weights carry (and the sums), so that p of rows of V that are very small or large throughout stays in the range of an fp32
+    // a power of two that weights carry (and the sums), so that p of rows of V that are very small or large throughout stays in the range of an fp32
     float unit = 1.f;
-    // the run's own blocks (kRT = 1: from the last key group on, the first ones have one more of the cache's if any)
+    // the run's own blocks (from the last wavefront on: the first ones have one more of the cache's if any)
     auto own_blocks = [&] {
-        int j = max(first, p.n_cache_blocks) + (kShared ? kg : kKG - 1 - kg) - p.n_cache_blocks;
+        int j = max(first, p.n_cache_blocks) + kWaves - 1 - (int)wave - p.n_cache_blocks;
         const int own_end = end - p.n_cache_blocks;
         if (j >= own_end) return;
         const char *const k = p.k + (int64_t)g * 256, *const v = p.v + (int64_t)g * 256;
         bf16x8 keys[2][4];
         ask_own_keys(keys, k, row_bytes, j, p.T, i16, h);
-        for (; j < own_end; j += kKG) attend_own(st, keys, k, v, row_bytes, j, kKG, p.T, query, p.scale_log2e, last, kShared ? 1.f : unit, i16, h);
+        for (; j < own_end; j += kWaves) attend_own(st, keys, k, v, row_bytes, j, kWaves, p.T, query, p.scale_log2e, last, unit, i16, h);
     };
-    int b = first + kg;  // the block that this wavefront is at
-    if constexpr (kShared) {
-        raw16 k{}, v{}, k1{}, v1{};
-        unsigned pair = 0, pair1 = 0;
-        auto ask = [&](int block) {  // a quarter of a block (behind the last one: that one again)
-            const char* const blk = base + min(block, stop - 1) * stride;
-            k = *reinterpret_cast<const raw16*>(blk + rt * 1024 + lane * 16);
-            v = *reinterpret_cast<const raw16*>(blk + kBlockV + rt * 1024 + lane * 16);
-            pair = *reinterpret_cast<const unsigned*>(blk + kBlockScales + 4 * (lane & 31));
-        };
-        auto widen_into = [&](int buffer) {
-            char* const to = smem + (2 * buffer + kg) * kStaged;
-            char* const mine = to + rt * 2048 + lane * 16;
-            *reinterpret_cast<f16x8*>(mine) = keys_of(k[0], k[1]);
-            *reinterpret_cast<f16x8*>(mine + 1024) = keys_of(k[2], k[3]);
-            *reinterpret_cast<bf16x8*>(mine + 8192) = values_of(v[0], v[1]);
-            *reinterpret_cast<bf16x8*>(mine + 9216) = values_of(v[2], v[3]);
-            // (by all four, the same)
-            *reinterpret_cast<float*>(to + 16384 + 4 * lane) = __uint_as_float(lane < 32 ? pair << 16 : pair & 0xffff0000u);
-        };
-        if (first < stop) {
-            ask(b + 2);
-            k1 = k, v1 = v, pair1 = pair;
-            ask(b);
-        }
-        own_blocks();  // (first: their queries are there as they are needed, and the cache's first blocks come meanwhile)
-        if (first < stop) {
-            const Queries q[2] = {queries_of(query[0], p.scale_log2e), queries_of(query[1], p.scale_log2e)};
-            widen_into(0);
-            k = k1, v = v1, pair = pair1;
-            __syncthreads();
-            if (kg == 1) __syncthreads();  // half a turn behind the other group
-            const int turns = (stop - first + 1) / 2;
-            f32x4 s[2][2];
-            bf16x8 weights[2];
-            int next = 1;
-            const char* block = smem + kg * kStaged;
-            multiply_keys(s, q, [&](int kt, int i) { return *reinterpret_cast<const f16x8*>(block + (4 * kt + i) * 1024 + lane * 16); });
-            widen_into(next);
-            ask(b + 4);
-            for (int turn = 0; turn < turns; ++turn, b += 2) {
-                __syncthreads();
-                f32x4 ks[2], vs[2];
+    int b = first + wave;  // the block that this wavefront is at
+    // the next block is asked for piece by piece as this one's are used up
+    raw16 k[4]{}, v[4]{}, pairs[2]{};
+    const char* blk = base + b * stride;
+    auto ask_keys = [&] {
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
-                    ks[kt] = *reinterpret_cast<const f32x4*>(block + 16384 + 64 * kt + 16 * h);
-                    vs[kt] = *reinterpret_cast<const f32x4*>(block + 16384 + 128 + 64 * kt + 16 * h);
-                }
-                raw16 piece[16];  // of V, then of the next block's K
-                const char* const after = smem + (2 * next + kg) * kStaged;
-                auto take = [&](int i) {
-                    piece[i] = *reinterpret_cast<const raw16*>(i < 8 ? block + 8192 + i * 1024 + lane * 16 : after + (i - 8) * 1024 + lane * 16);
-                };
-                weigh(st, weights, s, ks, vs, q, b < stop ? p.len - b * kBlockRows : 0, h, [&] {  // (no block is left: none of its rows count)
-                    __builtin_amdgcn_sched_barrier(0);
+        for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const raw16*>(blk + j * 1024 + lane * 16);
+    };
+    auto ask_values = [&] {
 #pragma unroll
-                    for (int i = 0; i < kAhead; ++i) take(i);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-                __syncthreads();
-                // The products, in this order: pieces come from LDS kAhead steps before they are multiplied, and a word is widened at a step.
-                __builtin_amdgcn_s_setprio(1);
-                next = next == 2 ? 0 : next + 1;
-                char* const to = smem + (2 * next + kg) * kStaged;
-                char* const mine = to + rt * 2048 + lane * 16;
-                const unsigned minus128 = 0xc300c300u;
-                const bf16x8 off = __builtin_bit_cast(bf16x8, u32x4{minus128, minus128, minus128, minus128});
+        for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const raw16*>(blk + kBlockV + j * 1024 + lane * 16);
+    };
+    auto ask_scales = [&] {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) st.excess[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(off, weights[c], st.excess[c], 0, 0, 0);
-                f32x4 fresh[2][2];
+        for (int kt = 0; kt < 2; ++kt) pairs[kt] = *reinterpret_cast<const raw16*>(blk + kBlockScales + 64 * kt + 16 * h);
+    };
+    Queries q[2];
+    if (b < stop) {
+        ask_scales();
+        ask_keys();
+        ask_values();
+        q[0] = queries_of(query[0], p.scale_log2e);
+        q[1] = queries_of(query[1], p.scale_log2e);
+        unsigned top = 0;  // the largest scale of V in the wavefront's first block (as a bit pattern, K's below it)
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) fresh[kt][c] = f32x4{q[c].start, q[c].start, q[c].start, q[c].start};
-                u32x4 wide;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    // (K's pieces come in the order (kt, step) 0 0, 0 1, .., 1 3)
-                    if (i + kAhead < 16) take(i + kAhead);
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (i < 8) st.o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, piece[i]), weights[c], st.o[c][i], 0, 0, 0);
-                        else {
-                            const int kt = (i - 8) >> 2, step = (i - 8) & 3;
-                            fresh[kt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, piece[i]), q[c].q[step], fresh[kt][c], 0, 0, 0);
-                        }
-                    }
-                    if (i < 8) {
-                        unsigned lo, hi;
-                        if (i < 4) widen_key(k[i], lo, hi);
-                        else widen(v[i - 4], lo, hi);
-                        wide[2 * (i & 1)] = lo;
-                        wide[2 * (i & 1) + 1] = hi;
-                        if (i & 1) *reinterpret_cast<u32x4*>(mine + (i < 4 ? 0 : 8192) + ((i >> 1) & 1) * 1024) = wide;
-                    } else if (i == 8) {
-                        *reinterpret_cast<float*>(to + 16384 + 4 * lane) = __uint_as_float(lane < 32 ? pair << 16 : pair & 0xffff0000u);
-                    } else if (i == 9) {
-                        ask(b + 6);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) s[kt][c] = fresh[kt][c];
-                block = after;
-                __builtin_amdgcn_s_setprio(0);
-            }
-            if (kg == 0) __syncthreads();
-        }
-    } else {
-        // the next block is asked for piece by piece as this one's are used up
-        raw16 k[4]{}, v[4]{}, pairs[2]{};
-        const char* blk = base + b * stride;
-        auto ask_keys = [&] {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const raw16*>(blk + j * 1024 + lane * 16);
-        };
-        auto ask_values = [&] {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const raw16*>(blk + kBlockV + j * 1024 + lane * 16);
-        };
-        auto ask_scales = [&] {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) pairs[kt] = *reinterpret_cast<const raw16*>(blk + kBlockScales + 64 * kt + 16 * h);
-        };
-        Queries q[2];
-        if (b < stop) {
-            ask_scales();
-            ask_keys();
-            ask_values();
-            q[0] = queries_of(query[0], p.scale_log2e);
-            q[1] = queries_of(query[1], p.scale_log2e);
-            unsigned top = 0;  // the largest scale of V in the wavefront's first block (as a bit pattern, K's below it)
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) top = max(top, 16 * kt + 4 * h + r < p.len - b * kBlockRows ? pairs[kt][r] : 0u);
-            top = __builtin_amdgcn_readfirstlane(over_rows(top, [](unsigned x, unsigned y) { return max(x, y); }));
-            if (top < __float_as_uint(0x1p-60f) && top >= __float_as_uint(0x1p-125f)) unit = 0x1p40f;  // (2^-126: rows of zeros)
-            else if (top > __float_as_uint(0x1p60f) && top < 0x7f800000u) unit = 0x1p-40f;
-        }
-        for (; b < stop; b += kKG) {
-            if (b + kKG < stop) blk += kKG * stride;  // (behind the last one: that one again)
-            f32x4 s[2][2], ks[2], vs[2];
-            f16x8 weights[2];
-            multiply_keys(s, q, [&](int kt, int i) { return keys_of(k[2 * kt + (i >> 1)][2 * (i & 1)], k[2 * kt + (i >> 1)][2 * (i & 1) + 1]); });
-            ask_keys();
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    ks[kt][r] = __uint_as_float(pairs[kt][r] << 16);
-                    vs[kt][r] = __uint_as_float(pairs[kt][r] & 0xffff0000u) * unit;
-                }
-            weigh_for_fp16(st, weights, s, ks, vs, q, p.len - b * kBlockRows, h);
-            const unsigned minus1152 = 0xe480e480u;
-            const f16x8 off = __builtin_bit_cast(f16x8, u32x4{minus1152, minus1152, minus1152, minus1152});
-#pragma unroll
-            for (int c = 0; c < 2; ++c) st.excess[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, weights[c], st.excess[c], 0, 0, 0);
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) {
-                const f16x8 a = keys_of(v[dt >> 1][2 * (dt & 1)], v[dt >> 1][2 * (dt & 1) + 1]);  // (code + 1152, as K's)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) st.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, weights[c], st.o[c][dt], 0, 0, 0);
-            }
-            ask_values();
-            ask_scales();
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-            if (st.limit[c] != -INFINITY) st.limit[c] = kLazyOwn;
-        own_blocks();
+            for (int r = 0; r < 4; ++r) top = max(top, 16 * kt + 4 * h + r < p.len - b * kBlockRows ? pairs[kt][r] : 0u);
+        top = __builtin_amdgcn_readfirstlane(over_rows(top, [](unsigned x, unsigned y) { return max(x, y); }));
+        if (top < __float_as_uint(0x1p-60f) && top >= __float_as_uint(0x1p-125f)) unit = 0x1p40f;  // (2^-126: rows of zeros)
+        else if (top > __float_as_uint(0x1p60f) && top < 0x7f800000u) unit = 0x1p-40f;
     }
+    for (; b < stop; b += kWaves) {
+        if (b + kWaves < stop) blk += kWaves * stride;  // (behind the last one: that one again)
+        f32x4 s[2][2], ks[2], vs[2];
+        f16x8 weights[2];
+        multiply_keys(s, q, [&](int kt, int i) { return keys_of(k[2 * kt + (i >> 1)][2 * (i & 1)], k[2 * kt + (i >> 1)][2 * (i & 1) + 1]); });
+        ask_keys();
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                ks[kt][r] = __uint_as_float(pairs[kt][r] << 16);
+                vs[kt][r] = __uint_as_float(pairs[kt][r] & 0xffff0000u) * unit;
+            }
+        weigh(st, weights, s, ks, vs, q, p.len - b * kBlockRows, h);
+        const unsigned minus1152 = 0xe480e480u;
+        const f16x8 off = __builtin_bit_cast(f16x8, u32x4{minus1152, minus1152, minus1152, minus1152});
+#pragma unroll
+        for (int c = 0; c < 2; ++c) st.excess[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, weights[c], st.excess[c], 0, 0, 0);
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            const f16x8 a = keys_of(v[dt >> 1][2 * (dt & 1)], v[dt >> 1][2 * (dt & 1) + 1]);  // (code + 1152, as K's)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) st.o[c][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, weights[c], st.o[c][dt], 0, 0, 0);
+        }
+        ask_values();
+        ask_scales();
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+        if (st.limit[c] != -INFINITY) st.limit[c] = kLazyOwn;
+    own_blocks();
 
-    // ---- the key groups meet in LDS, then 16 rows of a wavefront are done ----
+    // ---- the wavefronts' sums meet in LDS ----
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         st.l[c] = sum_over_rows(st.l[c]);
         if (st.limit[c] == -INFINITY) st.m[c] = -INFINITY;
+        float* const to = box + (2 * wave + c) * kBox;
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) st.o[c][dt] += st.excess[c];
-    }
-    if (!kShared && unit != 1.f) {
-        const float back = unit > 1.f ? 0x1p-40f : 0x1p40f;
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) st.o[c][dt] *= back;
-    }
-    __syncthreads();  // (blocks may still be read there)
-    float* const box = reinterpret_cast<float*>(smem);
-    // a set of columns of a wavefront in LDS: [dim % 8][lane][r], then references and sums
-    constexpr int kBox = 8 * 64 * 4 + 32;
-    auto put = [&](int slot, const f32x4 (&o)[8], float m, float l) {
-        float* const to = box + slot * kBox;
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(to + (dt * 64 + lane) * 4) = o[dt];
-        if (h == 0) {
-            to[2048 + i16] = m;
-            to[2064 + i16] = l;
+        for (int dt = 0; dt < 8; ++dt) {
+            f32x4 o = st.o[c][dt] + st.excess[c];
+            if (unit != 1.f) o *= unit > 1.f ? 0x1p-40f : 0x1p40f;
+            *reinterpret_cast<f32x4*>(to + (dt * 64 + lane) * 4) = o;
         }
-    };
-    auto add = [&](f32x4 (&o)[8], float& m, float& l, int slot) {
-        const float* const from = box + slot * kBox;
-        const float m2 = from[2048 + i16], mx = fmaxf(m, m2);
-        const float a = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx), b2 = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx);
-        m = mx;
-        l = l * a + from[2064 + i16] * b2;
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) o[dt] = o[dt] * a + *reinterpret_cast<const f32x4*>(from + (dt * 64 + lane) * 4) * b2;
-    };
+        if (h == 0) {
+            to[2048 + i16] = st.m[c];
+            to[2064 + i16] = st.l[c];
+        }
+    }
+    __syncthreads();
     // 8 values of a row, dims 32 hs + 8 r .. (hs: any quarter), times inv, to the output or, times 2^(se - 127), to the split's partial results
     auto store = [&](int row, int hs, int r, const float (&o)[8], float inv, int se) {
         if (row >= p.M) return;
@@ -594,61 +427,34 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
     auto exponent_of = [](float big) {  // (2^126 at most: its inverse is a number too)
         return min(max(127 + 14 + 127 - (int)((__float_as_uint(big) >> 23) & 255u), 1), 253);
     };
-    if constexpr (kShared) {  // each group of two does one set of columns
-        if (kg == 0) put(wave, st.o[1], st.m[1], st.l[1]);
-        else put(wave, st.o[0], st.m[0], st.l[0]);
-        __syncthreads();
-        if (kg == 1) {
+    // a wavefront adds half the dims of one set in the order of the wavefronts, a lane 8 (lane % 4) .. of a quarter's 32 of column lane / 4
+    const int set = wave & 1, column = lane >> 2, row = row0 + 16 * set + column;
+    const float* const from = box + set * kBox;
+    float f[kWaves], l = 0.f, mx = -INFINITY;
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) st.o[0][dt] = st.o[1][dt];
-            st.m[0] = st.m[1];
-            st.l[0] = st.l[1];
-        }
-        add(st.o[0], st.m[0], st.l[0], (wave + kRT) % kWaves);
-        const int row = row0 + 16 * kg + i16;
-        float big = 0.f;
+    for (int n = 0; n < kWaves; ++n) {
+        f[n] = from[2 * n * kBox + 2048 + column];
+        mx = fmaxf(mx, f[n]);
+    }
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt)
+    for (int n = 0; n < kWaves; ++n) {
+        // (the sum in two steps, as in weigh)
+        const float half = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (f[n] - mx));
+        l += half * from[2 * n * kBox + 2064 + column] * half;
+        f[n] = half * half;
+    }
+    const float inv = inverse_of(l);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) big = fmaxf(big, fabsf(st.o[0][dt][r]));
-        const float inv = inverse_of(st.l[0]);
-        const int se = exponent_of(big * inv);
+    for (int quarter = wave >> 1; quarter < 4; quarter += kWaves / 2) {
+        float o[8] = {}, big = 0.f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float o[8];
+        for (int n = 0; n < kWaves; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = st.o[0][e][r];
-            store(row, h, r, o, inv, se);
-        }
-        store_sums(row, h, st.m[0], st.l[0], se);
-    } else {
-        // every wavefront leaves both, and adds 32 dims of one set in the order of the groups, a lane dims 8 (lane % 4) .. of column lane / 4 (two
-        // wavefronts with a set each: 1 us more)
-        put(2 * wave, st.o[0], st.m[0], st.l[0]);
-        put(2 * wave + 1, st.o[1], st.m[1], st.l[1]);
-        __syncthreads();
-        const int set = wave & 1, quarter = wave >> 1, column = lane >> 2, row = row0 + 16 * set + column;
-        const float* const from = box + set * kBox;
-        float m[kWaves], l = 0.f, o[8] = {};
-#pragma unroll
-        for (int n = 0; n < kWaves; ++n) m[n] = from[2 * n * kBox + 2048 + column];
-        float mx = m[0];
-#pragma unroll
-        for (int n = 1; n < kWaves; ++n) mx = fmaxf(mx, m[n]);
-#pragma unroll
-        for (int n = 0; n < kWaves; ++n) {
-            // (the sum in two steps, as in weigh_for_fp16)
-            const float half = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (m[n] - mx)), f = half * half;
-            l += half * from[2 * n * kBox + 2064 + column] * half;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) o[dt] += f * from[2 * n * kBox + dt * 256 + quarter * 64 + lane];
-        }
-        float big = 0.f;
+            for (int dt = 0; dt < 8; ++dt) o[dt] += f[n] * from[2 * n * kBox + dt * 256 + quarter * 64 + lane];
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) big = fmaxf(big, fabsf(o[dt]));
         big = fmaxf(big, neighbour<0xb1>(big));  // of the four lanes of a column
         big = fmaxf(big, neighbour<0x4e>(big));
-        const float inv = inverse_of(l);
         const int se = exponent_of(big * inv);
         store(row, quarter, lane & 3, o, inv, se);
         if ((lane & 3) == 0) store_sums(row, quarter, mx, l, se);
@@ -686,7 +492,7 @@ __global__ __launch_bounds__(256) void prefill8_combine_kernel(Prefill8Params p)
 #pragma unroll
         for (int u = 0; u < kDepth; ++u) {
             if (s0 + u >= p.nsplit) continue;
-            // (in two steps, as in weigh_for_fp16)
+            // (in two steps, as in weigh)
             const float half = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (ml[u].x - mx)), w = half * ml[u].y * half, wo = w * __uint_as_float((254 - se[u]) << 23);
             l += w;
 #pragma unroll
@@ -701,37 +507,23 @@ __global__ __launch_bounds__(256) void prefill8_combine_kernel(Prefill8Params p)
     *reinterpret_cast<bf16x8*>(p.out + ((int64_t)t * p.Hq + (int64_t)g * p.G + row - t * p.G) * D + d8) = r;
 }
 
-// Row tiles per workgroup, row groups, and workgroups that share a group's keys.
+// Row tiles, and workgroups that share a tile's keys.
 struct Plan {
-    int rt, groups, nsplit;
+    int tiles, nsplit;
     int most;  // splits that no run of as many tokens over fewer rows passes
 };
 Plan plan_of(const vs_shape& s, int32_t n_tokens, int32_t len) {
-    const int G = s.n_q_heads / s.n_kv_heads, tiles = (n_tokens * G + kTileRows - 1) / kTileRows;
-    const int cached = (len + kBlockRows - 1) / kBlockRows, own = (n_tokens + 31) / 32;
-    Plan pl{};
-    pl.most = 1;
+    const int G = s.n_q_heads / s.n_kv_heads, tiles = (n_tokens * G + kTileRows - 1) / kTileRows, units = tiles * s.n_kv_heads;
+    const int blocks = (len + kBlockRows - 1) / kBlockRows + (n_tokens + 31) / 32;
+    Plan pl{tiles, 1, std::max(1, std::min({512 / units, blocks / kWaves, kMaxSplits}))};
+    // The number of splits by what a call takes, in us, from what was measured: a workgroup alone on a compute unit, or two, by what it takes at all and each
+    // of its blocks; and the launch that adds splits.  By splits, 28/4 heads: 37 tokens over 711 rows 10.4 at 1, 12.0 at 3; 64 over 3000 23.3 at 1, 16.6 at
+    // 4, 18.4 at 9; 1 over 4000 28.1 at 1, 13.1 at 6, 14.7 at 32; 100 over 4000 29.6 at 1, 24.1 at 2, 22.1 at 5; 170 over 2400 21.6 at 1, 22.4 at 3; over 4416 32.7 at 1, 33.1 at 2, 28.4 at 3.
     float least = INFINITY;
-    auto consider = [&](int rt, int groups, int nsplit, float us) {
-        if (us >= least) return;
-        least = us, pl.rt = rt, pl.groups = groups, pl.nsplit = nsplit;
-    };
-    auto way = [&](int rt, float group, float block, float own_block) {
-        const int groups = (tiles + rt - 1) / rt, units = groups * s.n_kv_heads;
-        const float blocks = cached + own_block * own;
-        const int n = std::max(1, std::min({256 / units, (cached + own) * rt / kWaves, kMaxSplits}));
-        consider(rt, groups, 1, 3.5f + ((units + 255) / 256) * (group + block * blocks));
-        if (n > 1) consider(rt, groups, n, 3.5f + group + block * blocks / n + 5.0f);
-        pl.most = std::max(pl.most, n);
-    };
-    // What a call takes, in us, from what was measured: a launch, what a workgroup takes besides its blocks, and each of its blocks, as often
-    // as workgroups follow one another on a compute unit; or as many splits as run at once, a block for every key group at least,
-    // and the launch that adds them.  One tile a workgroup has no merge where four have one; four spend fewer instructions on a block.
-    // Attention and merge, us, one tile / four, tokens x rows: 28/4 heads 10x200 8.5 / 12.4, 37x711 11.7 / 18.0, 64x1500 16.1 / 21.0,
-    // 100x8000 32.8 / 33.3, 170x352 11.0 / 20.4, 170x2400 20.4 / 26.2, 170x4416 29.1 / 32.1, 170x7000 40.5 / 39.4, 170x11016 58.0 / 50.5,
-    // 600x1000 42.7 / 45.6, 1024x0 45.5 / 41.8; 64/8 heads 300x300 28.8 / 24.6, 2048x200 269 / 227; 8/1 heads 170x11016 24.8 / 29.4.
-    way(1, 5.1f, 0.144f, 1.0f);
-    way(4, 10.2f, 0.525f, 1.25f);  // (causal: the longest of a group's rows count)
+    for (int n = 1; n <= pl.most; ++n) {
+        const float us = (units * n <= 256 ? 6.8f + 0.183f * blocks / n : 10.8f + 0.262f * blocks / n) + (n > 1 ? 4.5f + 0.1f * n : 0.0f);
+        if (us < least) least = us, pl.nsplit = n;
+    }
     return pl;
 }
 size_t partial_bytes(const vs_shape& s, int32_t n_tokens, int nsplit) {
@@ -765,7 +557,7 @@ hipError_t launch_prefill8(const vs_shape& s, void* cache, int32_t len, const vo
     p.Hkv = s.n_kv_heads;
     p.M = n_tokens * p.G;
     p.n_cache_blocks = (len + kBlockRows - 1) / kBlockRows;
-    p.n_groups = pl.groups;
+    p.n_tiles = pl.tiles;
     p.nsplit = pl.nsplit;
     p.scale_log2e = s.softmax_scale * kLog2e;
     p.part_ml = (char*)workspace;
@@ -774,9 +566,8 @@ hipError_t launch_prefill8(const vs_shape& s, void* cache, int32_t len, const vo
     p.first_kept = first_kept;
     p.n_keeping = first_kept < n_tokens ? ((len + n_tokens - first_kept - 1) / kBlockRows - len / kBlockRows + 1) * p.Hkv : 0;
     const int per_plane = pl.nsplit * p.Hkv * kWaves;
-    const dim3 grid(pl.nsplit, p.Hkv, pl.groups + (p.n_keeping + per_plane - 1) / per_plane);
-    if (pl.rt == 1) prefill8_kernel<1><<<grid, kThreads, 0, st>>>(p);
-    else prefill8_kernel<4><<<grid, kThreads, 0, st>>>(p);
+    const dim3 grid(pl.nsplit, p.Hkv, pl.tiles + (p.n_keeping + per_plane - 1) / per_plane);
+    prefill8_kernel<<<grid, kThreads, 0, st>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.nsplit == 1) return e;
     prefill8_combine_kernel<<<(p.M * p.Hkv + 15) / 16, 256, 0, st>>>(p);
