@@ -5,8 +5,8 @@
 // that one multiplies while the other starts or ends.  us by workgroup, 28/4 heads, 37 tokens over 711 rows, 170 over 11016, 600 over 1000, 2048 over 200:
 //   4 wavefronts 10.4, 47.4, 31.8, 95;  8, one workgroup to a compute unit 11.8, 58.2, 43.2, 125;  2 12.4, 48.8, 35.2, 97;
 //   8 of 128 rows that share a block, widened once, through LDS 17.4, 51.2, 45.8, 128.
-// Bound by vector instructions (some 200 of a block's turn, beside 34 matrix instructions, two wavefronts a SIMD; 170 over 11016 in three splits is
-// 650 TFLOP/s) and, for few blocks, by some 7 us of start and end: launch, first trips to memory, the queries' conversion, the sums' way
+// Bound by vector instructions (some 200 of a block's turn, beside 34 matrix instructions, two wavefronts a SIMD; 170 over 11016 in three splits 45.8 us =
+// 591 TFLOP/s, and 4.7 to add them) and, for few blocks, by some 7 us of start and end: launch, first trips to memory, the queries' conversion, the sums' way
 // through LDS, stores.
 #include "vs_cache8_attn.h"
 
