@@ -20,9 +20,13 @@ struct RowsParams {
     LenTable at;          // the cache's row that the first of them is
 };
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// What the code in the low byte stands for (15 + 8 bits: exact before the rounding).
+__device__ __forceinline__ __bf16 row_value(unsigned code, float scale) { return (__bf16)((float)((int)(code & 255u) - 128) * scale); }
+
 // A wavefront per (block, KV head), four a workgroup: the quantiser's lanes keep a row's maximum in 16 lanes and end up with whole words of the block
-// (vs_cache8.h), so that nothing passes through LDS.  Bound by memory for many rows (4 caches x 11016 rows of 4 heads, 136 MB: 26.8 us = 5.1 TB/s),
-// by the chain load, maximum, divide, store for few (28 caches x 1 row 4.9 us, x 37 rows 6.6 us).
+// (vs_cache8.h), so that nothing passes through LDS.  Bound by memory (4 caches x 11016 rows of 4 heads, 136 MB: 26.8 us = 5.1 TB/s).
 __global__ __launch_bounds__(kThreads) void cache8_append_kernel(RowsParams p) {
     const int lane = threadIdx.x & 63, item = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int at = p.at.v[blockIdx.y], block = at / kBlockRows + item / p.Hkv, g = item % p.Hkv;
@@ -32,7 +36,24 @@ __global__ __launch_bounds__(kThreads) void cache8_append_kernel(RowsParams p) {
                 at + p.n_rows, lane);
 }
 
-// The lanes of write_block the other way round.  136 MB as above: 22.4 us = 6.1 TB/s; 28 caches x 1 row 3.7 us, x 37 rows 5.6 us.
+// 16 lanes per (row, KV head): a row's codes of V go out byte by byte, so that nothing of the block is read.  Bound by the launch and the
+// chain load, maximum, divide, store.
+__global__ __launch_bounds__(kThreads) void cache8_append_rows_kernel(RowsParams p) {
+    const int c = threadIdx.x & 15, item = blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
+    if (item >= p.n_rows * p.Hkv) return;
+    const int n = item / p.Hkv, g = item - n * p.Hkv, at = p.at.v[blockIdx.y] + n, key = at % kBlockRows;
+    const int64_t src = blockIdx.y * p.rows_stride + ((int64_t)(p.first + n) * p.Hkv + g) * 256 + 16 * c;
+    char* const blk = p.slab + blockIdx.y * p.cache_bytes + ((int64_t)(at / kBlockRows) * p.Hkv + g) * kBlockBytes;
+    uint2 k_codes;
+    unsigned v_codes[8];
+    const unsigned pair = quantise(*reinterpret_cast<const raw16*>(p.k + src), *reinterpret_cast<const raw16*>(p.v + src), k_codes, v_codes);
+    *reinterpret_cast<uint2*>(blk + k_code_offset(key, c)) = k_codes;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) blk[v_code_offset(key, c, j)] = (char)v_codes[j];
+    if (c == 0) *reinterpret_cast<unsigned*>(blk + kBlockScales + 4 * key) = pair;
+}
+
+// The lanes of write_block the other way round.  136 MB as above: 22.4 us = 6.1 TB/s.
 __global__ __launch_bounds__(kThreads) void cache8_read_kernel(RowsParams p) {
     const int lane = threadIdx.x & 63, item = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, h = lane >> 4;
@@ -49,7 +70,6 @@ __global__ __launch_bounds__(kThreads) void cache8_read_kernel(RowsParams p) {
     for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const raw16*>(blk + kBlockV + j * 1024 + lane * 16);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) s[kt] = *reinterpret_cast<const raw16*>(blk + kBlockScales + 64 * kt + 16 * h);
-    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
         const int row = row0 + 16 * (u >> 2) + 4 * h + (u & 3);
@@ -60,15 +80,43 @@ __global__ __launch_bounds__(kThreads) void cache8_read_kernel(RowsParams p) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const unsigned kw = j < 4 ? k[u].x : k[u].y;
-            kx[j] = (__bf16)((float)((int)((kw >> (8 * (j & 3))) & 255u) - 128) * ks);  // (15 + 8 bits: exact before the rounding)
+            kx[j] = row_value(kw >> (8 * (j & 3)), ks);
             const unsigned vw = v[j >> 1][2 * (j & 1) + (u >> 2)];
-            vx[j] = (__bf16)((float)((int)((vw >> (8 * (u & 3))) & 255u) - 128) * vs);
+            vx[j] = row_value(vw >> (8 * (u & 3)), vs);
         }
         const int64_t at = dst + (int64_t)(row - first + p.first) * p.Hkv * 256;
         *reinterpret_cast<bf16x8*>(p.k + at) = kx;
         *reinterpret_cast<bf16x8*>(p.v + at) = vx;
     }
 }
+
+// 16 lanes per (row, KV head), as for few rows written.
+__global__ __launch_bounds__(kThreads) void cache8_read_rows_kernel(RowsParams p) {
+    const int c = threadIdx.x & 15, item = blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
+    if (item >= p.n_rows * p.Hkv) return;
+    const int n = item / p.Hkv, g = item - n * p.Hkv, at = p.at.v[blockIdx.y] + n, key = at % kBlockRows;
+    const char* const blk = p.slab + blockIdx.y * p.cache_bytes + ((int64_t)(at / kBlockRows) * p.Hkv + g) * kBlockBytes;
+    const uint2 k = *reinterpret_cast<const uint2*>(blk + k_code_offset(key, c));
+    const unsigned pair = *reinterpret_cast<const unsigned*>(blk + kBlockScales + 4 * key);
+    unsigned char v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const unsigned char*>(blk + v_code_offset(key, c, j));
+    const float ks = __uint_as_float(pair << 16), vs = __uint_as_float(pair & 0xffff0000u);
+    bf16x8 kx, vx;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        kx[j] = row_value((j < 4 ? k.x : k.y) >> (8 * (j & 3)), ks);
+        vx[j] = row_value(v[j], vs);
+    }
+    const int64_t dst = blockIdx.y * p.rows_stride + ((int64_t)(p.first + n) * p.Hkv + g) * 256 + 16 * c;
+    *reinterpret_cast<bf16x8*>(p.k + dst) = kx;
+    *reinterpret_cast<bf16x8*>(p.v + dst) = vx;
+}
+
+// Few rows go one by one, many in blocks.  us written and read, caches x KV heads x rows, one by one / in blocks: 28 x 4 x 1 2.9, 2.6 / 4.4, 3.8;
+// 28 x 4 x 37 4.3, 3.9 / 6.6, 5.4; 28 x 8 x 64 6.7, 6.1 / 7.0, 6.3; 4 x 4 x 1000 6.9, 6.1 / 6.9, 6.3; 28 x 4 x 170 7.8, 7.0 / 7.1, 6.5;
+// 4 x 4 x 2000 11.3, 8.9 / 7.8, 7.5.
+bool by_rows(const vs_shape& s, int32_t n_caches, int32_t n_rows) { return (int64_t)n_caches * n_rows * s.n_kv_heads <= 16384; }
 
 // (block, KV head) pairs that n_rows rows of any of the caches can touch
 int items_of(const vs_shape& s, int32_t n_caches, const LenTable& at, int32_t n_rows) {
@@ -99,6 +147,10 @@ RowsParams rows_params(const vs_shape& s, int32_t n_caches, const void* slab, in
 hipError_t launch_cache8_append(const vs_shape& s, int32_t n_caches, void* slab, int32_t capacity, const LenTable& lens, const void* k_rows,
                                 const void* v_rows, int32_t n_tokens, int32_t first_kept, hipStream_t st) {
     const RowsParams p = rows_params(s, n_caches, slab, capacity, lens, k_rows, v_rows, n_tokens, first_kept, n_tokens - first_kept);
+    if (by_rows(s, n_caches, p.n_rows)) {
+        cache8_append_rows_kernel<<<dim3((p.n_rows * p.Hkv + 15) / 16, n_caches), kThreads, 0, st>>>(p);
+        return hipGetLastError();
+    }
     cache8_append_kernel<<<dim3((p.items + 3) / 4, n_caches), kThreads, 0, st>>>(p);
     return hipGetLastError();
 }
@@ -106,6 +158,10 @@ hipError_t launch_cache8_append(const vs_shape& s, int32_t n_caches, void* slab,
 hipError_t launch_cache8_read(const vs_shape& s, int32_t n_caches, const void* slab, int32_t capacity, const LenTable& first, int32_t n_rows,
                               void* k_out, void* v_out, hipStream_t st) {
     const RowsParams p = rows_params(s, n_caches, slab, capacity, first, k_out, v_out, n_rows, 0, n_rows);
+    if (by_rows(s, n_caches, p.n_rows)) {
+        cache8_read_rows_kernel<<<dim3((p.n_rows * p.Hkv + 15) / 16, n_caches), kThreads, 0, st>>>(p);
+        return hipGetLastError();
+    }
     cache8_read_kernel<<<dim3((p.items + 3) / 4, n_caches), kThreads, 0, st>>>(p);
     return hipGetLastError();
 }

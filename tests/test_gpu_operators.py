@@ -173,6 +173,31 @@ def test_rows_written_and_read_back(hq, hkv, before, T, first):
         assert same_bits(k3[i], ko[i, firsts[i]:firsts[i] + some]) and same_bits(v3[i], vo[i, firsts[i]:firsts[i] + some])
 
 
+@pytest.mark.parametrize("hq,hkv,T,first", [(28, 4, 1400, 0), (8, 8, 701, 1), (5, 5, 1111, 7)])
+def test_many_rows_written_and_read_back(hq, hkv, T, first):
+    """As many as go in blocks, behind rows that end anywhere in one, of which nothing else may change; the same bytes as written row by row."""
+    sh, lens0, kept = vs.Shape.make(hq, hkv, 128, "bf16"), [5, 32, 63], T - first
+    cap = 64 + T
+    k, v = rows(120, 3, T, hkv, 128), rows(121, 3, T, hkv, 128)
+    slab, lens = slab_of(sh, 3, cap, fill=0x5A), lens_array(lens0)
+    one = slab.clone()
+    vs.cache8_append(sh, slab, cap, lens, k, v, first_kept=first)
+    assert list(lens) == [n + kept for n in lens0]
+    for i, n0 in enumerate(lens0):
+        part, n = one[i], lens_array([n0])
+        for t in range(first, T, 300):
+            e = min(t + 300, T)
+            vs.cache8_append(sh, part, cap, n, k[i:i + 1, t:e].contiguous(), v[i:i + 1, t:e].contiguous())
+    assert same_bits(slab, one)
+    ko, vo = (torch.empty((3, kept, hkv, 128), dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    vs.cache8_read(sh, slab, cap, lens, lens_array(lens0), ko, vo)
+    assert torch.equal(ko.cpu(), held(k[:, first:])) and torch.equal(vo.cpu(), held(v[:, first:]))
+    kr, vr = (torch.empty((3, 9, hkv, 128), dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    at = 700 - first - 20
+    vs.cache8_read(sh, slab, cap, lens, lens_array([n + at for n in lens0]), kr, vr)
+    assert same_bits(kr, ko[:, at:at + 9]) and same_bits(vr, vo[:, at:at + 9])
+
+
 def test_many_caches_of_different_lengths_and_a_longer_capacity():
     sh, n, T = vs.Shape.make(8, 2, 128, "bf16"), 131, 5
     before = [(7 * i) % 90 for i in range(n)]
