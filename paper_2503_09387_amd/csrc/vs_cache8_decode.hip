@@ -10,7 +10,6 @@ namespace {
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int D = 128;
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kRowStride = D + 4;  // of a query head's sums in LDS, in floats
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazyMax = 8.0f;  // scores may exceed the reference maximum by 2^8 before it is refreshed
@@ -173,7 +172,9 @@ __device__ __forceinline__ void add_shares(const Decode8Params& p, int s, int g,
 // the last to arrive adds the shares in index order, and nobody waits.  The upper 24 bits of a counter are a mark that
 // vs_workspace_init puts there; where they are something else the stream's first share does the whole stream.  Streams of many shares (counters
 // null) are added by a second launch.
-__global__ __launch_bounds__(kThreads, 2) void decode8_kernel(Decode8Params p) {
+template <int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void decode8_kernel(Decode8Params p) {
+    constexpr int kThreads = 64 * kWaves;
     __shared__ __attribute__((aligned(16))) float s_o[kWaves][kMaxGroup][kRowStride];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     __shared__ unsigned s_before;
@@ -310,19 +311,25 @@ __global__ __launch_bounds__(64) void decode8_shares_kernel(Decode8Params p) {
     if (n_shares > 1) add_shares<false>(p, s, g, first_share, n_shares, blockIdx.y - g * p.G, 2 * threadIdx.x);
 }
 
-constexpr int kMaxWorkgroups = 2048 / kWaves;
+constexpr int kMaxWorkgroups = 256;
 constexpr int kMaxSharesInside = 12, kMaxBlocksInside = 80, kAloneBlocks = 16;
+constexpr int kSmallBlocks = 32, kSmallWorkgroups = 128;
 
-// Blocks per share.  us a step, 28/4 heads:
-//   * up to 16 blocks a stream (2 a wavefront) one share and no merge: 1 x 256 rows 6.1 (shares of 8: 7.0), 1 x 380 6.4 (8.0), 1 x 500 7.25 (8.0);
-//     beyond, shares: 1 x 700 8.6 as one and 8.0 in shares of 8;
-//   * the fewest, from a block per wavefront on, with which all shares run at once, a workgroup per compute unit;
+// Wavefronts of a workgroup, and blocks per share.  us a step, 28/4 heads:
+//   * up to 16 blocks a stream one share and no merge: 1 x 256 rows 5.8 (in shares 7.0), 1 x 380 6.2 (7.4), 1 x 500 7.1 (7.4); beyond, shares: 1 x 700
+//     8.5 as one and 7.3 in shares;
+//   * 4 wavefronts and shares of 4 blocks while a stream has 32 at most and that makes 128 workgroups at most: 1 x 700 7.3 (8 wavefronts 7.9),
+//     1 x 1000 7.3 (8.0), 4 x 700 7.9 (8.1); beyond, 8: 16 x 700 9.2 (4 wavefronts 10.0), 1 x 1400 8.0 (9.5), 16 ragged 20.9 (24.3);
+//   * with 8, the fewest shares, from a block per wavefront on, with which all run at once, a workgroup per compute unit;
 //   * but at most 12 shares, which the last to arrive adds, as long as they are no more than 80 blocks: 1 x 8192 12.3 (32 shares and a second
 //     launch 15.1), 1 x 16384 15.2 (19.9), 1 x 32768 22.8 (22.9), 1 x 50000 30.2 (25.1).
 // Streams that do not fit all at once are not shared out.
 // 16 streams of 640..8320 rows (78.9 MB): 19.0 us = 4.2 TB/s, of which some 4 us are the launch, the first trip to memory and the merge; in between
 // bytes come at a large copy's rate.
-int blocks_per_share(const LenTable& lens, int n_streams, int n_kv_heads) {
+struct Plan {
+    int waves, per_share;
+};
+Plan plan_of(const LenTable& lens, int n_streams, int n_kv_heads) {
     auto blocks_of = [&](int i) { return (lens.v[i] + kBlockRows - 1) / kBlockRows; };
     int64_t total = 0;
     int most = 0;
@@ -330,16 +337,17 @@ int blocks_per_share(const LenTable& lens, int n_streams, int n_kv_heads) {
         total += blocks_of(i);
         most = std::max(most, blocks_of(i));
     }
-    if (most <= kAloneBlocks || (int64_t)n_streams * n_kv_heads >= kMaxWorkgroups) return most;
+    if (most <= kSmallBlocks && (int64_t)n_streams * n_kv_heads * ((most + 3) / 4) <= kSmallWorkgroups) return {4, most <= kAloneBlocks ? most : 4};
+    if (most <= kAloneBlocks || (int64_t)n_streams * n_kv_heads >= kMaxWorkgroups) return {8, most};
     auto fits = [&](int c) {
         int64_t n = 0;
         for (int i = 0; i < n_streams; ++i) n += (blocks_of(i) + c - 1) / c;
         return n * n_kv_heads <= kMaxWorkgroups;
     };
-    int c = (int)std::min<int64_t>(std::max<int64_t>(total * n_kv_heads / kMaxWorkgroups, kWaves), most);
+    int c = (int)std::min<int64_t>(std::max<int64_t>(total * n_kv_heads / kMaxWorkgroups, 8), most);
     while (c < most && !fits(c)) c += 1 + c / 32;
     const int inside = (most + kMaxSharesInside - 1) / kMaxSharesInside;
-    return std::min(inside <= kMaxBlocksInside ? std::max(c, inside) : c, most);
+    return {8, std::min(inside <= kMaxBlocksInside ? std::max(c, inside) : c, most)};
 }
 
 }  // namespace
@@ -363,7 +371,8 @@ hipError_t launch_decode8(const vs_shape& s, int32_t n_streams, void* slab, int3
     p.Hkv = s.n_kv_heads;
     p.scale_log2e = s.softmax_scale * kLog2e;
     p.lens = lens;
-    const int c = blocks_per_share(lens, n_streams, s.n_kv_heads);
+    const Plan pl = plan_of(lens, n_streams, s.n_kv_heads);
+    const int c = pl.per_share;
     int n = 0, most = 0;
     for (int i = 0; i < kMaxStreamsPerLaunch; ++i) {
         const int of = i < n_streams ? ((lens.v[i] + kBlockRows - 1) / kBlockRows + c - 1) / c : 0;
@@ -375,7 +384,8 @@ hipError_t launch_decode8(const vs_shape& s, int32_t n_streams, void* slab, int3
     p.part_ml = (float*)workspace;
     p.part_o = p.part_ml + (int64_t)kMaxWorkgroups * p.G * 2;
     p.counters = most <= kMaxSharesInside ? (unsigned*)counters : nullptr;
-    decode8_kernel<<<dim3(n, s.n_kv_heads), kThreads, 0, st>>>(p);
+    if (pl.waves == 4) decode8_kernel<4><<<dim3(n, s.n_kv_heads), 256, 0, st>>>(p);
+    else decode8_kernel<8><<<dim3(n, s.n_kv_heads), 512, 0, st>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || n == n_streams || p.counters) return e;
     decode8_shares_kernel<<<dim3(n_streams, s.n_q_heads), 64, 0, st>>>(p);
