@@ -76,8 +76,11 @@ __device__ __forceinline__ Queries queries_of(const raw16 (&w)[4], float scale_l
         for (int j = 0; j < 4; ++j) most = max_pairs(most, w[i][j] & 0x7fff7fffu);
     most = max(most & 0xffffu, most >> 16);
     most = over_rows(most, [](unsigned a, unsigned b) { return max(a, b); });
-    // (up to 2^126: the smallest bf16 is then 2^-7, an fp16 like any other)
-    const int up = min(14 + 127 - (int)(most >> 7), 126);
+    // (Up to 2^126, and no further than scale_log2e 2^-up is an fp32 with all its bits: at the scale of Eq. 1 2^123, which makes the
+    // smallest bf16 2^-10, an fp16 like any other.  A smaller scale may hold up back further: 128 values of the query are then off by 2^(-25 - up) each
+    // at most, which over the largest keys, 2^128, is 2^-15 of a score.)
+    const int most_up = min((int)((__float_as_uint(scale_log2e) >> 23) & 255u) - 1, 126);
+    const int up = min(14 + 127 - (int)(most >> 7), most_up);
     const float factor = __uint_as_float((unsigned)(127 + up) << 23);
     const unsigned minus1152 = 0xe480e480u;
     const f16x8 off = __builtin_bit_cast(f16x8, u32x4{minus1152, minus1152, minus1152, minus1152});
@@ -93,8 +96,8 @@ __device__ __forceinline__ Queries queries_of(const raw16 (&w)[4], float scale_l
         start = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, out.q[i], start, 0, 0, 0);
     }
     out.start = start[0];
-    // (a query that is not finite gives scores that are not numbers; a factor of 0 would make them of what is masked)
-    out.f = most > 0x7f7fu ? __uint_as_float(0x7fc00000u) : fmaxf(ldexpf(scale_log2e, -up), 1.17549435e-38f);
+    // (a query that is not finite gives scores that are not numbers)
+    out.f = most > 0x7f7fu ? __uint_as_float(0x7fc00000u) : ldexpf(scale_log2e, -up);
     return out;
 }
 

@@ -722,3 +722,28 @@ def test_more_than_4_gib_of_rows():
             terms = far / 64                                # of one lane, if a single wavefront took an eighth of the rows
             bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + np.expm1(2 * e) + terms * 2.0 ** -24) * 1.01 * absolute + 2.0 ** -15 * absolute.max()
             assert (np.abs(f64(out[i, h]) - want) <= bound).all(), (i, h)
+
+
+# ---------------------------------------------------------------------------- the ends of the range
+@pytest.mark.parametrize("q_up,k_up,scale_up", [(-112, 112, 0), (-109, 109, 0), (-122, 118, 0), (-60, 118, -57), (-20, 118, -97), (112, -112, 0), (60, -90, 28)])
+def test_small_queries_over_large_keys_and_the_reverse(q_up, k_up, scale_up):
+    """Q, K and the softmax scale times powers of two: the scores stay of ordinary size, and so does what a score may be off (see
+    decode_bound).  Tokens over cached rows, over their own rows, and a step."""
+    sh = vs.Shape.make(8, 2, 128, "bf16", 128 ** -0.5 * 2.0 ** scale_up)
+    scale, L, T = float(np.float32(sh.softmax_scale)), 300, 40
+    k, v = rows(130, 1, L, 2, 128, loud=False) * 2.0 ** k_up, rows(131, 1, L, 2, 128)
+    q, kt, vt = rows(132, T, 8, 128, loud=False, sigma=2.0) * 2.0 ** q_up, rows(133, T, 2, 128, loud=False) * 2.0 ** k_up, rows(134, T, 2, 128)
+    slab, lens = slab_of(sh, 1, L + T), lens_array([0])
+    vs.cache8_append(sh, slab, L + T, lens, k, v)
+    ws = vs.make_cache8_workspace(sh, T, L + T, 1, DEV)
+    out = torch.full_like(q, float("nan"))
+    vs.cache8_prefill_attn(sh, vs.Cache8(slab[0], L + T, L), q, kt, vt, out, ws, first_kept=T)
+    kk, vv = (np.concatenate([ref.stands_for(f64(a[0])), f64(b)]) for a, b in ((k, kt), (v, vt)))
+    for t in (0, 3, 39):
+        want, absolute, most = ref.attend(f64(q[t:t + 1]), kk, vv, [L + t + 1], scale)
+        bound = ref.prefill_bound(f64(q[t]), kk[:L + t + 1], vv[:L + t + 1], want[0], absolute[0], most[0], scale)
+        err = np.abs(f64(out[t]) - want[0])
+        assert np.isfinite(err).all() and (err <= bound).all(), f"token {t}: {(err / bound).max():.2f}"
+    step = torch.full_like(q[:1], float("nan"))
+    vs.cache8_decode_attn(sh, slab, L + T, lens, q[:1], kt[:1], vt[:1], step, ws)
+    check_decode(sh, step, 0, q[:1], k, v, kt[:1], vt[:1], L, "step")
