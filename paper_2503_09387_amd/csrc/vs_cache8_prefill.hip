@@ -22,6 +22,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazyMax = 8.0f;     // scores may exceed the reference maximum by 2^8 before it is refreshed
 constexpr float kMaxWeight = 15.0f;  // log2 of the largest weight that goes into an fp16
 constexpr float kLazyOwn = 20.0f;    // as kLazyMax for a run's own rows, behind cached ones whose weights have set the reference
+constexpr unsigned kLargeOwn = (127 + 60) << 7;  // 2^60, a bf16
 constexpr int kMaxSplits = 32;
 
 struct Prefill8Params {
@@ -49,21 +50,25 @@ struct State {
     float limit[2];    // what weights, of a run's own rows scores, may come to before the reference is refreshed, log2: -INFINITY until a key has been seen
 };
 
-// Scores less the reference become probabilities; the sums take them.
-__device__ __forceinline__ void soften(State& st, float (&x)[2][8]) {
+// A value that all lanes have, in a scalar register.
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
+// Scores less the reference become probabilities; the sums take them.  room: log2 of what probabilities may come to beside these values.
+__device__ __forceinline__ void soften(State& st, float (&x)[2][8], float room) {
     const float mx[2] = {max_of_8(x[0]), max_of_8(x[1])};
-    if (__any(mx[0] > st.limit[0] || mx[1] > st.limit[1])) {  // rare after the first block
+    if (__any(mx[0] > fminf(st.limit[0], room) || mx[1] > fminf(st.limit[1], room))) {  // rare after the first block
         asm volatile("s_nop 15\n\ts_nop 15");  // (the last matrix instruction's sums, before assembly that the compiler does not look into)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const bool seen = st.limit[c] != -INFINITY;
-            float up = max_over_rows(mx[c]);
+            float up = max_over_rows(mx[c]) - fminf(room, 0.f);
             if (seen) up = fmaxf(up, 0.f);
             if (up == -INFINITY) up = 0.f;  // (the column sees none of these keys and has seen none before)
             else st.limit[c] = kLazyMax;
-            const float keep = seen ? __builtin_amdgcn_exp2f(-up) : 1.f;
+            // (in two steps, as in weigh)
+            const float half = seen ? __builtin_amdgcn_exp2f(-0.5f * up) : 1.f, keep = half * half;
             st.m[c] += up;
-            st.l[c] *= keep;
+            st.l[c] = st.l[c] * half * half;
             scale_in_place(st.excess[c], keep);
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) scale_in_place(st.o[c][dt], keep);
@@ -158,6 +163,33 @@ __device__ __forceinline__ void weigh(State& st, f16x8 (&w)[2], const f32x4 (&s)
         }
 }
 
+// The largest scale of V (as a bit pattern, K's below it) of a wavefront's blocks b, b + kWaves, ..: 8 lanes take a block's 32 pairs,
+// kScanDepth times 8 blocks from number n on.
+constexpr int kScanDepth = 4;
+__device__ __forceinline__ int scan_block(int b, int n, int u, int lane) { return b + (n + 8 * u + (lane >> 3)) * kWaves; }
+__device__ __forceinline__ void ask_block_scales(raw16 (&to)[kScanDepth], const char* scales, int64_t stride, int b, int n, int stop, int lane) {
+#pragma unroll
+    for (int u = 0; u < kScanDepth; ++u) to[u] = *reinterpret_cast<const raw16*>(scales + min(scan_block(b, n, u, lane), stop - 1) * stride + 16 * (lane & 7));
+}
+__device__ __forceinline__ unsigned top_of(const raw16 (&scales)[kScanDepth], int b, int n, int stop, int len, int lane) {
+    unsigned top = 0;
+#pragma unroll
+    for (int u = 0; u < kScanDepth; ++u) {
+        const int row = kBlockRows * scan_block(b, n, u, lane) + 4 * (lane & 7);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = max(top, row + r < len ? scales[u][r] : 0u);
+    }
+    return top;
+}
+// The largest of all lanes' values, in a scalar register.
+__device__ __forceinline__ unsigned over_lanes(unsigned x) {
+    x = over_rows(x, [](unsigned a, unsigned b) { return max(a, b); });
+    x = max(x, turned<8>(x));
+    x = max(x, turned<4>(x));
+    x = max(x, turned<2>(x));
+    return __builtin_amdgcn_readfirstlane(max(x, turned<1>(x)));
+}
+
 // The keys of a block of the run's own rows, keys 32 j .., as the products take them.
 __device__ __forceinline__ void ask_own_keys(bf16x8 (&to)[2][4], const char* k, int64_t row_bytes, int j, int T, int i16, int h) {
 #pragma unroll
@@ -167,9 +199,9 @@ __device__ __forceinline__ void ask_own_keys(bf16x8 (&to)[2][4], const char* k, 
         for (int i = 0; i < 4; ++i) to[kt][i] = *reinterpret_cast<const bf16x8*>(row + 64 * i);
     }
 }
-// Such a block: column c sees keys up to `last[c]` of the run; sums in units of 1 / unit.  The keys of block j + step are asked for on the way.
+// Such a block: column c sees keys up to `last[c]` of the run.  The keys of block j + step are asked for on the way.
 __device__ __forceinline__ void attend_own(State& st, bf16x8 (&keys)[2][4], const char* k, const char* v, int64_t row_bytes, int j, int step, int T,
-                                           const raw16 (&q)[2][4], float f, const int (&last)[2], float unit, int i16, int h) {
+                                           const raw16 (&q)[2][4], float f, const int (&last)[2], int i16, int h) {
     raw16 x[8];  // 8 keys, of each dims 8 i16 ..
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -199,12 +231,16 @@ __device__ __forceinline__ void attend_own(State& st, bf16x8 (&keys)[2][4], cons
     };
     // A value that is not finite must not reach the columns that do not see its key (0 times it is NaN): such values go in as 0,
     // and the columns that do see one become NaN there.
-    unsigned most = 0;
+    auto most_of = [](const raw16 (&w)[8]) {
+        unsigned most = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 8; ++e)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = max_pairs(most, x[e][i] & 0x7fff7fffu);
-    if (__any(max(most & 0xffffu, most >> 16) > 0x7f7fu)) {
+            for (int i = 0; i < 4; ++i) most = max_pairs(most, w[e][i] & 0x7fff7fffu);
+        return max(most & 0xffffu, most >> 16);
+    };
+    const unsigned most = most_of(x);
+    if (__any(most > 0x7f7fu)) {
         bf16x8 sees[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c)
@@ -235,12 +271,18 @@ __device__ __forceinline__ void attend_own(State& st, bf16x8 (&keys)[2][4], cons
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[e][i] &= ~bad(x[e][i]);
     }
-    soften(st, z);
+    // Values of 2^60 and more leave probabilities, which may stand at 2^20 and behind rows of smaller values higher, less room: products of at most
+    // 2^100, so that the sums over a run stay numbers.
+    float room = kLazyOwn;
+    if (__any(most >= kLargeOwn)) {
+        room = fminf(room, (float)(100 + 126 - (int)(over_lanes(most_of(x)) >> 7)));
+    }
+    soften(st, z, room);
     bf16x8 p[2];
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)(z[c][e] * unit);
+        for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)z[c][e];
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
         const bf16x8 a = columns_of(x, dt);
@@ -306,7 +348,9 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         for (int i = 0; i < 4; ++i) query[c][i] = *reinterpret_cast<const raw16*>(at + 64 * i);
         last[c] = t;
     }
-    // a power of two that weights carry (and the sums), so that p of rows of V that are very small or large throughout stays in the range of an fp32
+    // a power of two that weights over cached rows carry (and the sums), so that their p stay in the range of an fp32, with room for smaller ones, whatever
+    // the size of V.  It goes by the largest scale in all of the wavefront's blocks, which are looked through while the first block and the queries
+    // are on their way: small rows may come first and far larger ones behind them.
     float unit = 1.f;
     // the run's own blocks (from the last wavefront on: the first ones have one more of the cache's if any)
     auto own_blocks = [&] {
@@ -316,7 +360,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         const char *const k = p.k + (int64_t)g * 256, *const v = p.v + (int64_t)g * 256;
         bf16x8 keys[2][4];
         ask_own_keys(keys, k, row_bytes, j, p.T, i16, h);
-        for (; j < own_end; j += kWaves) attend_own(st, keys, k, v, row_bytes, j, kWaves, p.T, query, p.scale_log2e, last, unit, i16, h);
+        for (; j < own_end; j += kWaves) attend_own(st, keys, k, v, row_bytes, j, kWaves, p.T, query, p.scale_log2e, last, i16, h);
     };
     int b = first + wave;  // the block that this wavefront is at
     // the next block is asked for piece by piece as this one's are used up
@@ -336,19 +380,21 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
     };
     Queries q[2];
     if (b < stop) {
+        raw16 scales[kScanDepth];
+        ask_block_scales(scales, base + kBlockScales, stride, b, 0, stop, lane);
         ask_scales();
         ask_keys();
         ask_values();
         q[0] = queries_of(query[0], p.scale_log2e);
         q[1] = queries_of(query[1], p.scale_log2e);
-        unsigned top = 0;  // the largest scale of V in the wavefront's first block (as a bit pattern, K's below it)
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = max(top, 16 * kt + 4 * h + r < p.len - b * kBlockRows ? pairs[kt][r] : 0u);
-        top = __builtin_amdgcn_readfirstlane(over_rows(top, [](unsigned x, unsigned y) { return max(x, y); }));
-        if (top < __float_as_uint(0x1p-60f) && top >= __float_as_uint(0x1p-125f)) unit = 0x1p40f;  // (2^-126: rows of zeros)
-        else if (top > __float_as_uint(0x1p60f) && top < 0x7f800000u) unit = 0x1p-40f;
+        unsigned top = top_of(scales, b, 0, stop, p.len, lane);
+        for (int n = 8 * kScanDepth; b + n * kWaves < stop; n += 8 * kScanDepth) {
+            ask_block_scales(scales, base + kBlockScales, stride, b, n, stop, lane);
+            top = max(top, top_of(scales, b, n, stop, p.len, lane));
+        }
+        top = over_lanes(top);
+        if (top < __float_as_uint(0x1p-60f)) unit = 0x1p40f;
+        else if (top > __float_as_uint(0x1p90f)) unit = 0x1p-40f;
     }
     for (; b < stop; b += kWaves) {
         if (b + kWaves < stop) blk += kWaves * stride;  // (behind the last one: that one again)
@@ -377,6 +423,16 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         ask_values();
         ask_scales();
     }
+    if (unit != 1.f) {  // (the run's own rows have none)
+        asm volatile("s_nop 15\n\ts_nop 15");  // (as in soften)
+        const float back = unit > 1.f ? 0x1p-40f : 0x1p40f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            scale_in_place(st.excess[c], back);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) scale_in_place(st.o[c][dt], back);
+        }
+    }
 #pragma unroll
     for (int c = 0; c < 2; ++c)
         if (st.limit[c] != -INFINITY) st.limit[c] = kLazyOwn;
@@ -390,9 +446,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefill8_kernel(Prefill8Params p)
         float* const to = box + (2 * wave + c) * kBox;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) {
-            f32x4 o = st.o[c][dt] + st.excess[c];
-            if (unit != 1.f) o *= unit > 1.f ? 0x1p-40f : 0x1p40f;
-            *reinterpret_cast<f32x4*>(to + (dt * 64 + lane) * 4) = o;
+            *reinterpret_cast<f32x4*>(to + (dt * 64 + lane) * 4) = st.o[c][dt] + st.excess[c];
         }
         if (h == 0) {
             to[2048 + i16] = st.m[c];

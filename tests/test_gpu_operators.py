@@ -50,6 +50,14 @@ def held(x):
     return torch.from_numpy(ref.stands_for(f64(x)).astype(np.float32)).to(torch.bfloat16)
 
 
+def off_by(out, want):
+    """What the values are off; a value past the largest bf16 by less than half a step is an infinity when it is rounded."""
+    got = f64(out)
+    most = float(torch.finfo(torch.bfloat16).max)
+    got = np.where(np.isinf(got) & (np.abs(want) >= most * (1 - 2.0 ** -9)), np.sign(got) * most, got)
+    return np.where(np.isfinite(got), np.abs(got - want), np.inf)
+
+
 # ---------------------------------------------------------------------------- rotary positions
 def rotary_bound(x, ref_y, pos, dtype):
     """The revolutions are off by 3 roundings of 2^-53 of themselves (rate, product, 2 pi) and, in fp32, by 2^-26: an angle by 2 pi times
@@ -747,3 +755,72 @@ def test_small_queries_over_large_keys_and_the_reverse(q_up, k_up, scale_up):
     step = torch.full_like(q[:1], float("nan"))
     vs.cache8_decode_attn(sh, slab, L + T, lens, q[:1], kt[:1], vt[:1], step, ws)
     check_decode(sh, step, 0, q[:1], k, v, kt[:1], vt[:1], L, "step")
+
+
+@pytest.mark.parametrize("hq,hkv,L,T", [(8, 2, 300, 40), (8, 2, 1000, 3), (28, 4, 300, 400), (28, 4, 9000, 170)])
+def test_prefill_where_one_side_is_far_larger(hq, hkv, L, T):
+    """V of the run and of the cache, and of a cache's first and last rows, tens of powers of two apart, either way round; up to the largest bf16."""
+    s = AttnShape(hq, hkv, 128, "bf16")
+    sh = vs_shape(s)
+    k, v = rows(140, 1, L, hkv, 128), rows(141, 1, L, hkv, 128, loud=False)
+    q, kt, vt = rows(142, T, hq, 128, loud=False, sigma=1.0), rows(143, T, hkv, 128, loud=False), rows(144, T, hkv, 128, loud=False)
+    row = torch.arange(L, device=DEV)[None, :, None, None]
+    late, one = row >= L // 2 + 5, row == L - 7
+    top = torch.full_like(vt, torch.finfo(torch.bfloat16).max)
+    top[:, :, ::2] *= -1
+    zeros = torch.where(row < 200, 0.0, v)
+    cases = {"own rows large": (v, vt * 2.0 ** 112), "own rows largest": (v, top), "all rows largest": (v * 0 + top[0, 0], top),
+             "own rows 2^140 up": (v * 2.0 ** -55, vt * 2.0 ** 85), "own rows 2^200 up": (v * 2.0 ** -100, vt * 2.0 ** 100),
+             "cached rows 2^200 up": (v * 2.0 ** 100, vt * 2.0 ** -100), "both large": (v * 2.0 ** 122, vt * 2.0 ** 122),
+             "own rows 2^60 up, both large": (v * 2.0 ** 62, vt * 2.0 ** 122), "last rows 2^180 up": (torch.where(late, v * 2.0 ** 100, v * 2.0 ** -80), vt),
+             "last rows 2^205 up": (torch.where(late, v * 2.0 ** 122, v * 2.0 ** -83), vt), "last rows 2^120 up": (torch.where(late, v * 2.0 ** 40, v * 2.0 ** -80), vt * 2.0 ** 40),
+             "one row 2^200 up": (torch.where(one, v * 2.0 ** 120, v * 2.0 ** -80), vt * 2.0 ** -80), "first rows zeros, last large": (torch.where(late, zeros * 2.0 ** 110, zeros), vt),
+             "first rows zeros, the others tiny": (zeros * 2.0 ** -105, vt * 2.0 ** -105), "last rows large, own larger": (torch.where(late, v * 2.0 ** 100, v), vt * 2.0 ** 120)}
+    ws = vs.make_cache8_workspace(sh, T, L, 0, DEV)
+    wrong = []
+    for name, (v1, vt1) in cases.items():
+        v1, vt1 = v1.to(torch.bfloat16), vt1.to(torch.bfloat16)
+        slab, lens = slab_of(sh, 1, L + T), lens_array([0])
+        vs.cache8_append(sh, slab, L + T, lens, k, v1)
+        out = torch.full_like(q, float("nan"))
+        vs.cache8_prefill_attn(sh, vs.Cache8(slab[0], L + T, L), q, kt, vt1, out, ws)
+        kk, vv = (np.concatenate([ref.stands_for(f64(a[0])), f64(b)]) for a, b in ((k, kt), (v1, vt1)))
+        for t in sorted({0, T // 2, T - 1}):
+            want, absolute, most = ref.attend(f64(q[t:t + 1]), kk, vv, [L + t + 1], scale32(s))
+            bound = ref.prefill_bound(f64(q[t]), kk[:L + t + 1], vv[:L + t + 1], want[0], absolute[0], most[0], scale32(s))
+            err = off_by(out[t], want[0])
+            if not (err <= bound).all():
+                wrong.append(f"{name}, token {t}: {(err / bound).max():.2f}")
+    assert not wrong, wrong
+
+
+@pytest.mark.parametrize("hq,hkv,L,T", [(8, 2, 300, 40), (28, 4, 9000, 170)])
+def test_prefill_with_large_rows_that_nobody_looks_at(hq, hkv, L, T):
+    """A cached row of 2^80, or an own one of 2^110, whose score is some 400 under the others': what is seen is 2^-40 and keeps its bits."""
+    s = AttnShape(hq, hkv, 128, "bf16")
+    sh = vs_shape(s)
+    g = torch.Generator(device=DEV).manual_seed(7)
+    k, v = rows(150, 1, L, hkv, 128, loud=False), rows(151, 1, L, hkv, 128, loud=False) * 2.0 ** -40
+    q, kt, vt = rows(152, T, hq, 128, loud=False, sigma=0.2), rows(153, T, hkv, 128, loud=False), rows(154, T, hkv, 128, loud=False) * 2.0 ** -40
+    q[..., 0] = 30.0
+    k[..., 0], kt[..., 0] = 0.0, 0.0
+    cached, own, own_large = (torch.randint(0, n, (2,), generator=g, device=DEV) for n in (L, T, T))
+    k2, v2, kt2, vt2 = k.clone(), v.clone(), kt.clone(), vt.clone()
+    k2[0, cached, :, 0] = -150.0                      # a score of -150 * 30 / sqrt(128) = -398
+    v2[0, cached] *= 2.0 ** 120
+    kt2[own_large, :, 0] = -150.0
+    vt2[own_large] = vt2[own_large] * 2.0 ** 75 * 2.0 ** 75
+    ws = vs.make_cache8_workspace(sh, T, L, 0, DEV)
+    for name, (k1, v1, kt1, vt1) in {"cached": (k2, v2, kt, vt), "own": (k, v, kt2, vt2), "both": (k2, v2, kt2, vt2)}.items():
+        slab, lens = slab_of(sh, 1, L + T), lens_array([0])
+        vs.cache8_append(sh, slab, L + T, lens, k1, v1)
+        out = torch.full_like(q, float("nan"))
+        vs.cache8_prefill_attn(sh, vs.Cache8(slab[0], L + T, L), q, kt1, vt1, out, ws, first_kept=T)
+        kk, vv = (np.concatenate([ref.stands_for(f64(a[0])), f64(b)]) for a, b in ((k1, kt1), (v1, vt1)))
+        for t in (0, T // 2, T - 1):
+            want, absolute, most = ref.attend(f64(q[t:t + 1]), kk, vv, [L + t + 1], scale32(s))
+            # (a key whose probability is under 2^-500 adds nothing, whatever became of it: the bounds without its value)
+            seen = np.abs(kk[:L + t + 1, 0, 0]) < 100
+            bound = ref.prefill_bound(f64(q[t]), kk[:L + t + 1], vv[:L + t + 1] * seen[:, None, None], want[0], absolute[0], most[0], scale32(s))
+            err = off_by(out[t], want[0])
+            assert (err <= bound).all(), f"{name}, token {t}: {(err / bound).max():.2f}"
