@@ -470,6 +470,10 @@ vs_status vs_rotary(const vs_shape *shape, const vs_rotary_plan *plan, const int
  * when it is written, by itself: len may be lowered to any number of rows and the cache grown again from there.  A row with
  * a value that is not finite stands for NaN in all its values.  bf16 shapes only (VS_ERR_UNSUPPORTED otherwise).
  *
+ * Attention over such rows takes K, V and queries of any size that a bf16 has, as long as the scores are in the range of an fp32 and
+ * softmax_scale times a query's values stays under 2^140.  An output is as good as its rounding, but where values of V over 2^90 are among
+ * the rows (seen with next to no weight), outputs under 2^-50 may lose bits or be 0.
+ *
  * A cache of `capacity` rows is vs_cache8_bytes(shape, capacity) bytes of device memory, 16-byte aligned (0: the shape is not
  * supported, or capacity < 1 or beyond 1 TiB).  It needs no preparation.  What lies in it is the library's business but for this: it begins with
  * the same bytes whatever the capacity, so the first vs_cache8_bytes(shape, len) bytes are a copy of the len rows.

@@ -13,6 +13,10 @@ constexpr int D = 128;
 constexpr int kRowStride = D + 4;  // of a query head's sums in LDS, in floats
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazyMax = 8.0f;  // scores may exceed the reference maximum by 2^8 before it is refreshed
+// Where the sums of p s_v come to 2^93, the wavefront begins again with a reference 2^48 up: probabilities are up to 2^8, codes 255 and scales of V
+// 2^121, and sums of that over the wavefronts of a stream would pass an fp32.  (What is below 2^-78 of the largest probability then counts as nothing:
+// that is at most 2^50 a key, where outputs are 2^93 over the sum of probabilities at least.)
+constexpr float kLargeExcess = 0x1p100f, kLift = 48.0f;
 
 struct Decode8Params {
     char* slab;
@@ -54,7 +58,7 @@ struct State {
 };
 
 // One block, of which `valid` rows are there.
-__device__ __forceinline__ void attend(State& st, const Block& b, const Queries& q, int valid, int h) {
+__device__ __forceinline__ void attend(State& st, const Block& b, const Queries& q, int valid, int h, float lift) {
     float z[8], sv[8];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -78,8 +82,8 @@ __device__ __forceinline__ void attend(State& st, const Block& b, const Queries&
             }
     }
     float mx = max_of_8(z);
-    if (__any(mx > st.m + kLazyMax)) {  // rare after the first block
-        mx = max_over_rows(mx);
+    if (__any(mx > st.m + (kLazyMax - lift))) {  // rare after the first block
+        mx = max_over_rows(mx) + lift;
         const float m_new = fmaxf(st.m, mx), alpha = __builtin_amdgcn_exp2f(st.m - m_new);  // 0 at first
         st.m = m_new;
         st.l *= alpha;
@@ -195,52 +199,59 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode8_kernel(Decode8Params p
     const unsigned per = (unsigned)n_blocks / n_shares, more = n_blocks - per * n_shares;
     const int first = j_share * per + min((unsigned)j_share, more), end = first + per + ((unsigned)j_share < more);
     State st;
+    int b;
+    for (float lift = 0.f;; lift = kLift) {  // (once, but for values near the largest: 0.1 .. 0.2 us a step)
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) st.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    st.excess = st.o[0];
-    st.m = -INFINITY;
-    st.l = 0.f;
-    int b = first + wave;
-    if (b < end) {
-        // (loads come back in order: the query and the new row before the blocks)
-        const char* const q_row = p.q + ((int64_t)s * p.Hq + (int64_t)g * p.G + min(i16, p.G - 1)) * 256 + 16 * h;
-        raw16 words[4];
+        for (int dt = 0; dt < 8; ++dt) st.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        st.excess = st.o[0];
+        st.m = -INFINITY;
+        st.l = 0.f;
+        b = first + wave;
+        if (b < end) {
+            // (loads come back in order: the query and the new row before the blocks)
+            int64_t from = 0;
+            asm volatile("" : "+s"(from));  // (or these loads, and what waits for them, leave the loop and come before the blocks are asked for: 0.2 us)
+            const char* const q_row = p.q + from + ((int64_t)s * p.Hq + (int64_t)g * p.G + min(i16, p.G - 1)) * 256 + 16 * h;
+            raw16 words[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) words[i] = *reinterpret_cast<const raw16*>(q_row + 64 * i);
-        // the step's new row, by the wavefront that attends over the block that it falls into: to memory, and into the block as it is here
-        const bool keeps = p.k_new && end == n_blocks && wave == (unsigned)(n_blocks - 1 - first) % kWaves;
-        const int64_t at = ((int64_t)s * p.Hkv + g) * 256 + 16 * i16;  // (asked for by all: behind a branch it would be waited for)
-        const raw16 k_new = *reinterpret_cast<const raw16*>((p.k_new ? p.k_new : p.q) + at), v_new = *reinterpret_cast<const raw16*>((p.k_new ? p.v_new : p.q) + at);
-        Block x, y;
-        const char* blk = base + b * stride;
-        fetch(x, blk, lane);
-        blk += kWaves * stride;
-        if (b + kWaves < end) fetch(y, blk, lane);
-        const Queries q = queries_of(words, p.scale_log2e);
-        uint2 k_codes{};
-        unsigned v_codes[8] = {}, pair = 0;
-        if (keeps) {
-            const int key = (len - 1) % kBlockRows;
-            pair = quantise(k_new, v_new, k_codes, v_codes);
-            if (h == 0) {
-                char* const to = base + (n_blocks - 1) * stride;
+            for (int i = 0; i < 4; ++i) words[i] = *reinterpret_cast<const raw16*>(q_row + 64 * i);
+            // the step's new row, by the wavefront that attends over the block that it falls into: to memory, and into the block as it is here
+            const bool keeps = p.k_new && end == n_blocks && wave == (unsigned)(n_blocks - 1 - first) % kWaves;
+            const int64_t at = from + ((int64_t)s * p.Hkv + g) * 256 + 16 * i16;  // (asked for by all: behind a branch it would be waited for)
+            const raw16 k_new = *reinterpret_cast<const raw16*>((p.k_new ? p.k_new : p.q) + at), v_new = *reinterpret_cast<const raw16*>((p.k_new ? p.v_new : p.q) + at);
+            Block x, y;
+            const char* blk = base + b * stride;
+            fetch(x, blk, lane);
+            blk += kWaves * stride;
+            if (b + kWaves < end) fetch(y, blk, lane);
+            const Queries q = queries_of(words, p.scale_log2e);
+            uint2 k_codes{};
+            unsigned v_codes[8] = {}, pair = 0;
+            if (keeps) {
+                const int key = (len - 1) % kBlockRows;
+                pair = quantise(k_new, v_new, k_codes, v_codes);
+                if (h == 0) {
+                    char* const to = base + (n_blocks - 1) * stride;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) to[v_code_offset(key, i16, j)] = (char)v_codes[j];
-                *reinterpret_cast<uint2*>(to + k_code_offset(key, i16)) = k_codes;
-                if (i16 == 0) *reinterpret_cast<unsigned*>(to + kBlockScales + 4 * key) = pair;
+                    for (int j = 0; j < 8; ++j) to[v_code_offset(key, i16, j)] = (char)v_codes[j];
+                    *reinterpret_cast<uint2*>(to + k_code_offset(key, i16)) = k_codes;
+                    if (i16 == 0) *reinterpret_cast<unsigned*>(to + kBlockScales + 4 * key) = pair;
+                }
+            }
+            auto turn = [&](Block& here) {
+                if (keeps && b + 1 == n_blocks) put_row(here, (len - 1) % kBlockRows, k_codes, v_codes, pair, i16, h);
+                attend(st, here, q, len - b * kBlockRows, h, lift);
+                b += kWaves;
+                blk += kWaves * stride;
+                if (b + kWaves < end) fetch(here, blk, lane);
+            };
+            while (b < end) {
+                turn(x);
+                if (b < end) turn(y);
             }
         }
-        auto turn = [&](Block& here) {
-            if (keeps && b + 1 == n_blocks) put_row(here, (len - 1) % kBlockRows, k_codes, v_codes, pair, i16, h);
-            attend(st, here, q, len - b * kBlockRows, h);
-            b += kWaves;
-            blk += kWaves * stride;
-            if (b + kWaves < end) fetch(here, blk, lane);
-        };
-        while (b < end) {
-            turn(x);
-            if (b < end) turn(y);
-        }
+        // (the excess is -128 times a column's sum of p s_v; or a row or query was not finite, and nothing changes)
+        if (lift > 0.f || !__any(!(st.excess[0] > -kLargeExcess))) break;
     }
     st.l = sum_over_rows(st.l);
     if (h == 0) {

@@ -824,3 +824,58 @@ def test_prefill_with_large_rows_that_nobody_looks_at(hq, hkv, L, T):
             bound = ref.prefill_bound(f64(q[t]), kk[:L + t + 1], vv[:L + t + 1] * seen[:, None, None], want[0], absolute[0], most[0], scale32(s))
             err = off_by(out[t], want[0])
             assert (err <= bound).all(), f"{name}, token {t}: {(err / bound).max():.2f}"
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 1), (28, 4)])
+@pytest.mark.parametrize("lens0", [[1, 40], [500, 3], [3000, 33, 700], [64000, 1]])
+def test_decode_of_values_up_to_the_largest(hq, hkv, lens0):
+    """Long flat keys over V near the largest bf16, throughout, in some rows, in the new row alone: a mean is no larger than what it is of."""
+    sh, slab, cap, lens, k, v, q, kn, vn = decode_case(hq, hkv, lens0, 160, loud=False)
+    ws = vs.make_cache8_workspace(sh, 0, cap, len(lens0), DEV)
+    row = torch.arange(k.shape[1], device=DEV)[None, :, None, None]
+    largest = torch.full_like(v, torch.finfo(torch.bfloat16).max)
+    rising = (k.float() + q.float()[:, None, ::hq // hkv] * row / k.shape[1] * 0.5).to(torch.bfloat16)
+    cases = {"flat, largest": (torch.ones_like(k), largest, torch.ones_like(kn), largest[:, 0]), "flat, 2^118": (torch.ones_like(k), v * 2.0 ** 118, kn, vn * 2.0 ** 118),
+             "2^122": (k, v * 2.0 ** 122, kn, vn * 2.0 ** 122), "rising scores, 2^122": (rising, v * 2.0 ** 122, kn, vn * 2.0 ** 122),
+             "new row alone": (k, v, kn, vn * 2.0 ** 122), "every other block": (k, torch.where(row // 32 % 2 == 1, v * 2.0 ** 120, v), kn, vn),
+             "last rows": (k, torch.where(row >= k.shape[1] // 2, v * 2.0 ** 120, v), kn, vn), "first rows": (k, torch.where(row < 70, v * 2.0 ** 120, v), kn, vn)}
+    wrong = []
+    for name, (k1, v1, kn1, vn1) in cases.items():
+        if lens0[0] > 10000 and name not in ("flat, largest", "2^122", "last rows"):
+            continue
+        k1, v1, kn1, vn1 = (t.to(torch.bfloat16) for t in (k1, v1, kn1, vn1))
+        lens = lens_array([0] * len(lens0))
+        vs.cache8_append(sh, slab, cap, lens, k1, v1)
+        for i, n in enumerate(lens0):
+            lens[i] = n
+        out = torch.full_like(q, float("nan"))
+        vs.cache8_decode_attn(sh, slab, cap, lens, q, kn1, vn1, out, ws)
+        scale = float(np.float32(sh.softmax_scale))
+        for i, n0 in enumerate(lens0):
+            kk, vv = (ref.stands_for(f64(torch.cat([a[i, :n0], b[i:i + 1]]))) for a, b in ((k1, kn1), (v1, vn1)))
+            want, absolute, most = ref.attend(f64(q[i:i + 1]), kk, vv, [n0 + 1], scale)
+            bound = ref.decode_bound(f64(q[i]), kk, vv, want[0], absolute[0], most[0], scale)
+            err = off_by(out[i], want[0])
+            if not (err <= bound).all():
+                wrong.append(f"{name}, stream {i}: {(err / bound).max():.2f}")
+    assert not wrong, wrong
+
+
+def test_decode_with_large_rows_that_nobody_looks_at():
+    """A row of 2^120 whose score is some 400 under the others', in one stream of two: what is seen is of ordinary size and keeps its bits."""
+    lens0 = [700, 90]
+    sh, slab, cap, lens, k, v, q, kn, vn = decode_case(28, 4, lens0, 170, loud=False)
+    ws = vs.make_cache8_workspace(sh, 0, cap, 2, DEV)
+    q[..., 0] = 30.0
+    k[..., 0], kn[..., 0] = 0.0, 0.0
+    k[:, [5, 69], :, 0] = -150.0                     # a score of -150 * 30 / sqrt(128) = -398
+    clean = v.clone()
+    v[:, [5, 69]] *= 2.0 ** 120
+    clean[:, [5, 69]] = 0.0
+    lens = lens_array([0, 0])
+    vs.cache8_append(sh, slab, cap, lens, k, v)
+    lens[0], lens[1] = lens0
+    out = torch.full_like(q, float("nan"))
+    vs.cache8_decode_attn(sh, slab, cap, lens, q, kn, vn, out, ws)
+    for i, n0 in enumerate(lens0):
+        check_decode(sh, out, i, q, k, clean, kn, vn, n0, f"stream {i}")
