@@ -24,9 +24,8 @@ namespace vs {
 constexpr int kBlockRows = 32;
 constexpr int kBlockV = 4096, kBlockScales = 8192, kBlockBytes = 8320;  // offsets in a block, and its size: a multiple of 128
 
-inline int64_t cache8_bytes(const vs_shape& s, int32_t capacity) {
-    return ((int64_t)capacity + kBlockRows - 1) / kBlockRows * s.n_kv_heads * kBlockBytes;
-}
+inline int blocks_of(int32_t rows) { return (int)(((int64_t)rows + kBlockRows - 1) / kBlockRows); }  // (for any number of rows)
+inline int64_t cache8_bytes(const vs_shape& s, int32_t capacity) { return (int64_t)blocks_of(capacity) * s.n_kv_heads * kBlockBytes; }
 
 // Where lane c of a row's 16 lanes (dims 8 c .. 8 c + 7) finds its 8 K codes of row `key` of a block.
 __device__ __forceinline__ int k_code_offset(int key, int c) {

@@ -341,7 +341,7 @@ struct Plan {
     int waves, per_share;
 };
 Plan plan_of(const LenTable& lens, int n_streams, int n_kv_heads) {
-    auto blocks_of = [&](int i) { return (lens.v[i] + kBlockRows - 1) / kBlockRows; };
+    auto blocks_of = [&](int i) { return vs::blocks_of(lens.v[i]); };
     int64_t total = 0;
     int most = 0;
     for (int i = 0; i < n_streams; ++i) {
@@ -386,7 +386,7 @@ hipError_t launch_decode8(const vs_shape& s, int32_t n_streams, void* slab, int3
     const int c = pl.per_share;
     int n = 0, most = 0;
     for (int i = 0; i < kMaxStreamsPerLaunch; ++i) {
-        const int of = i < n_streams ? ((lens.v[i] + kBlockRows - 1) / kBlockRows + c - 1) / c : 0;
+        const int of = i < n_streams ? (blocks_of(lens.v[i]) + c - 1) / c : 0;
         n += of;
         most = std::max(most, of);
         p.share_end[i] = i < n_streams ? n : 0x7fffffff;  // (never "before" a share)

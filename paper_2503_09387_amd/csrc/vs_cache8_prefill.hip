@@ -564,7 +564,7 @@ struct Plan {
 };
 Plan plan_of(const vs_shape& s, int32_t n_tokens, int32_t len) {
     const int G = s.n_q_heads / s.n_kv_heads, tiles = (n_tokens * G + kTileRows - 1) / kTileRows, units = tiles * s.n_kv_heads;
-    const int blocks = (len + kBlockRows - 1) / kBlockRows + (n_tokens + 31) / 32;
+    const int blocks = blocks_of(len) + blocks_of(n_tokens);
     Plan pl{tiles, 1, std::max(1, std::min({512 / units, blocks / kWaves, kMaxSplits}))};
     // The number of splits by what a call takes, in us, from what was measured: a workgroup alone on a compute unit, or two, by what it takes at all and each
     // of its blocks; and the launch that adds splits.  By splits, 28/4 heads: 37 tokens over 711 rows 10.4 at 1, 12.0 at 3; 64 over 3000 23.3 at 1, 16.6 at
@@ -606,7 +606,7 @@ hipError_t launch_prefill8(const vs_shape& s, void* cache, int32_t len, const vo
     p.Hq = s.n_q_heads;
     p.Hkv = s.n_kv_heads;
     p.M = n_tokens * p.G;
-    p.n_cache_blocks = (len + kBlockRows - 1) / kBlockRows;
+    p.n_cache_blocks = blocks_of(len);
     p.n_tiles = pl.tiles;
     p.nsplit = pl.nsplit;
     p.scale_log2e = s.softmax_scale * kLog2e;

@@ -161,6 +161,16 @@ def test_a_workspace_serves_any_run_over_fewer_rows(hq, hkv):
         assert sizes == sorted(sizes), rows
 
 
+@pytest.mark.parametrize("hq,hkv", [(28, 4), (8, 8), (8, 1)])
+def test_a_workspace_for_any_number_of_rows(hq, hkv):
+    """Up to the largest number of rows that can be asked for."""
+    s = _shape(hq, hkv)
+    for tokens in (1, 37, 170, 4096):
+        rows = [1000, 100_000, 2 ** 20, 2 ** 30, 2 ** 31 - 33, 2 ** 31 - 32, 2 ** 31 - 31, 2 ** 31 - 1]
+        sizes = [vs.cache8_workspace_bytes(s, tokens, r, 0) for r in rows]
+        assert sizes == sorted(sizes), (tokens, sizes)
+
+
 def test_cache8_append_and_read_argument_errors():
     L, s = vs.lib(), _shape()
 
