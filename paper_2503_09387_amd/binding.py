@@ -2,6 +2,7 @@
 prefix.  Tensors are torch CUDA(ROCm) tensors; the current torch stream is used unless
 one is given.  There is no fallback: if the library is missing, importing `lib()` raises."""
 import ctypes
+import functools
 import os
 
 VS_F32, VS_BF16 = 0, 1
@@ -162,12 +163,25 @@ def current_stream_handle():
 def _ws(workspace):
     if workspace is None:
         return None, 0
-    return _ptr(workspace), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def _check(rc, what):
     if rc != 0:
         raise VSError(rc, what)
+
+
+def _dense(t, n_bytes, what):
+    """The address of a tensor (or None) that has to be n_bytes, one behind the other."""
+    if t is None:
+        return None
+    if t.nbytes == n_bytes and t.is_contiguous():
+        return t.data_ptr()
+    raise VSError(2, f"{what}: a tensor of {tuple(t.shape)} {t.dtype} where {n_bytes} bytes in a row belong")
+
+
+def _head_bytes(shape):
+    return shape.head_dim * 4 if shape.dtype == VS_F32 else shape.head_dim * 2
 
 
 def workspace_bytes(shape, max_q_tokens, max_cache_rows, n_streams):
@@ -401,9 +415,12 @@ class RotaryPlan:
 
 def rotary(shape, plan, positions, q, k, q_out, k_out, inverse=False, stream=None):
     """positions: device int32 [3][T]; q, q_out [T][Hq][D], k, k_out [T][Hkv][D] (either pair may be None; in place: out is in)."""
-    assert positions.element_size() == 4 and positions.is_contiguous()
-    _check(lib().vs_rotary(ctypes.byref(shape), ctypes.byref(plan.c), _ptr(positions), positions.shape[1], _ptr(q), _ptr(k), bool(inverse),
-                           _ptr(q_out), _ptr(k_out), _stream(stream)), "vs_rotary")
+    assert positions.element_size() == 4 and not positions.is_floating_point()
+    what, n = "vs_rotary", positions.shape[1]
+    head = n * _head_bytes(shape)
+    nq, nk = shape.n_q_heads * head, shape.n_kv_heads * head
+    _check(lib().vs_rotary(ctypes.byref(shape), ctypes.byref(plan.c), _dense(positions, 12 * n, what), n, _dense(q, nq, what), _dense(k, nk, what),
+                           bool(inverse), _dense(q_out, nq, what), _dense(k_out, nk, what), _stream(stream)), what)
 
 
 class _CCache8(ctypes.Structure):
@@ -412,6 +429,20 @@ class _CCache8(ctypes.Structure):
 
 def cache8_bytes(shape, capacity):
     return int(lib().vs_cache8_bytes(ctypes.byref(shape), capacity))
+
+
+@functools.lru_cache(maxsize=1024)
+def _cache8_size(n_kv_heads, capacity):
+    return cache8_bytes(Shape.make(n_kv_heads, n_kv_heads, 128, VS_BF16), capacity)
+
+
+def _caches8(shape, n, slab, capacity, lens, what):
+    """The address of n caches of that capacity, which have to be in the tensor, with as many lengths."""
+    if slab.nbytes < n * _cache8_size(shape.n_kv_heads, capacity) or not slab.is_contiguous():
+        raise VSError(2, f"{what}: {slab.nbytes} bytes where {n} caches of {capacity} rows belong")
+    if len(lens) < n:
+        raise VSError(2, f"{what}: {len(lens)} lengths for {n} caches")
+    return slab.data_ptr()
 
 
 class Cache8:
@@ -454,30 +485,42 @@ def make_cache8_workspace(shape, max_q_tokens, max_cache_rows, n_streams, device
 def cache8_append(shape, slab, capacity, lens, k_rows, v_rows, first_kept=0, stream=None):
     """slab: uint8 [n_caches][cache8_bytes]; lens: ctypes int32 array [n_caches] (host), grown by the rows kept;
     k_rows, v_rows [n_caches][T][Hkv][D], rows first_kept.. of which are quantised into the caches."""
-    _check(lib().vs_cache8_append(ctypes.byref(shape), k_rows.shape[0], _ptr(slab), capacity, lens, _ptr(k_rows), _ptr(v_rows),
-                                  k_rows.shape[1], first_kept, _stream(stream)), "vs_cache8_append")
+    what, n, tokens = "vs_cache8_append", k_rows.shape[0], k_rows.shape[1]
+    nk = n * tokens * shape.n_kv_heads * _head_bytes(shape)
+    _check(lib().vs_cache8_append(ctypes.byref(shape), n, _caches8(shape, n, slab, capacity, lens, what), capacity, lens, _dense(k_rows, nk, what),
+                                  _dense(v_rows, nk, what), tokens, first_kept, _stream(stream)), what)
 
 
 def cache8_read(shape, slab, capacity, lens, first_rows, k_out, v_out, stream=None):
     """Rows first_rows[i].. (None: 0..) of every cache as what they stand for -> k_out, v_out [n_caches][n][Hkv][D]."""
-    _check(lib().vs_cache8_read(ctypes.byref(shape), k_out.shape[0], _ptr(slab), capacity, lens, first_rows, k_out.shape[1],
-                                _ptr(k_out), _ptr(v_out), _stream(stream)), "vs_cache8_read")
+    what, n, rows = "vs_cache8_read", k_out.shape[0], k_out.shape[1]
+    nk = n * rows * shape.n_kv_heads * _head_bytes(shape)
+    if first_rows is not None and len(first_rows) < n:
+        raise VSError(2, f"{what}: {len(first_rows)} first rows for {n} caches")
+    _check(lib().vs_cache8_read(ctypes.byref(shape), n, _caches8(shape, n, slab, capacity, lens, what), capacity, lens, first_rows, rows,
+                                _dense(k_out, nk, what), _dense(v_out, nk, what), _stream(stream)), what)
 
 
 def cache8_decode_attn(shape, slab, capacity, lens, q, k_new, v_new, out, workspace, stream=None):
     """decode_attn over a slab of caches in 8 bits; q, out [n_streams][Hq][D]."""
+    what, n = "vs_cache8_decode_attn", q.shape[0]
+    head = n * _head_bytes(shape)
+    nq, nk = shape.n_q_heads * head, shape.n_kv_heads * head
     wp, wb = _ws(workspace)
-    _check(lib().vs_cache8_decode_attn(ctypes.byref(shape), q.shape[0], _ptr(slab), capacity, lens, _ptr(q), _ptr(k_new), _ptr(v_new),
-                                       _ptr(out), wp, wb, _stream(stream)), "vs_cache8_decode_attn")
+    _check(lib().vs_cache8_decode_attn(ctypes.byref(shape), n, _caches8(shape, n, slab, capacity, lens, what), capacity, lens, _dense(q, nq, what),
+                                       _dense(k_new, nk, what), _dense(v_new, nk, what), _dense(out, nq, what), wp, wb, _stream(stream)), what)
 
 
 def cache8_prefill_attn(shape, cache, q, k_t, v_t, out, workspace, first_kept=None, stream=None):
     """A run's tokens over a Cache8; rows first_kept.. of the run (None: the last, the carrier) are quantised into it."""
+    what, n = "vs_cache8_prefill_attn", q.shape[0]
+    head = n * _head_bytes(shape)
+    nq, nk = shape.n_q_heads * head, shape.n_kv_heads * head
+    if cache.data.nbytes < _cache8_size(shape.n_kv_heads, cache.c.capacity):
+        raise VSError(2, f"{what}: {cache.data.nbytes} bytes where a cache of {cache.c.capacity} rows belongs")
     wp, wb = _ws(workspace)
-    n = q.shape[0]
-    _check(lib().vs_cache8_prefill_attn(ctypes.byref(shape), ctypes.byref(cache.c), _ptr(q), _ptr(k_t), _ptr(v_t), n,
-                                        n - 1 if first_kept is None else first_kept, _ptr(out), wp, wb, _stream(stream)),
-           "vs_cache8_prefill_attn")
+    _check(lib().vs_cache8_prefill_attn(ctypes.byref(shape), ctypes.byref(cache.c), _dense(q, nq, what), _dense(k_t, nk, what), _dense(v_t, nk, what), n,
+                                        n - 1 if first_kept is None else first_kept, _dense(out, nq, what), wp, wb, _stream(stream)), what)
 
 
 def carrier_mean_pool(e, c_out, dtype, stream=None):

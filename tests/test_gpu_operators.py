@@ -835,7 +835,7 @@ def test_decode_of_values_up_to_the_largest(hq, hkv, lens0):
     row = torch.arange(k.shape[1], device=DEV)[None, :, None, None]
     largest = torch.full_like(v, torch.finfo(torch.bfloat16).max)
     rising = (k.float() + q.float()[:, None, ::hq // hkv] * row / k.shape[1] * 0.5).to(torch.bfloat16)
-    cases = {"flat, largest": (torch.ones_like(k), largest, torch.ones_like(kn), largest[:, 0]), "flat, 2^118": (torch.ones_like(k), v * 2.0 ** 118, kn, vn * 2.0 ** 118),
+    cases = {"flat, largest": (torch.ones_like(k), largest, torch.ones_like(kn), largest[:, 0].contiguous()), "flat, 2^118": (torch.ones_like(k), v * 2.0 ** 118, kn, vn * 2.0 ** 118),
              "2^122": (k, v * 2.0 ** 122, kn, vn * 2.0 ** 122), "rising scores, 2^122": (rising, v * 2.0 ** 122, kn, vn * 2.0 ** 122),
              "new row alone": (k, v, kn, vn * 2.0 ** 122), "every other block": (k, torch.where(row // 32 % 2 == 1, v * 2.0 ** 120, v), kn, vn),
              "last rows": (k, torch.where(row >= k.shape[1] // 2, v * 2.0 ** 120, v), kn, vn), "first rows": (k, torch.where(row < 70, v * 2.0 ** 120, v), kn, vn)}

@@ -237,3 +237,51 @@ def test_cache8_prefill_argument_errors():
     assert pre(data=ODD) == 6 and pre(k=ODD) == 6 and pre(out=ODD) == 6 and pre(ws=ODD) == 6
     assert pre(ws=None) == 5 and pre(wsb=64) == 5 and need > 64
     assert pre(shape=_shape(4, 1, 64, vs.VS_F32)) == 3
+
+
+# ---------------------------------------------------------------------------- what the binding refuses
+def _refused(call, *args, **kwargs):
+    with pytest.raises(vs.VSError) as err:
+        call(*args, stream=0, **kwargs)
+    assert err.value.code == 2
+
+
+def test_binding_refuses_tensors_that_are_not_what_the_call_covers():
+    """Memory that is smaller than the capacity says, fewer lengths than caches, tensors of other sizes, types and strides than the others': found
+    before the library is called."""
+    torch = pytest.importorskip("torch")
+    s, n, cap, T = _shape(8, 2), 3, 40, 6
+    lens = (ctypes.c_int32 * n)(4, 4, 4)
+
+    def bf(*dims):
+        return torch.zeros(dims, dtype=torch.bfloat16)
+
+    slab, k, ws = torch.zeros((n, vs.cache8_bytes(s, cap)), dtype=torch.uint8), bf(n, T, 2, 128), torch.zeros(1 << 20, dtype=torch.uint8)
+    few, wide = (ctypes.c_int32 * 2)(4, 4), bf(n, T, 2, 256)[..., :128]
+    for bad in ((slab[:2], cap, lens, k, k), (slab, cap + 32, lens, k, k), (slab, cap, few, k, k), (slab, cap, lens, k, k[:, :5].contiguous()), (slab, cap, lens, k[..., :64].contiguous(), k),
+                (slab, cap, lens, k.float(), k.float()), (slab, cap, lens, k, wide), (slab[:, ::2], cap, lens, k, k), (slab, cap, lens, k[:1].expand(n, T, 2, 128), k)):
+        _refused(vs.cache8_append, s, *bad)
+    for bad in ((slab[:2], cap, lens, None, k, k), (slab, cap, few, None, k, k), (slab, cap, lens, few, k, k), (slab, cap, lens, None, k, k[:2].contiguous()), (slab, cap, lens, None, wide, k)):
+        _refused(vs.cache8_read, s, *bad)
+    q, kn = bf(n, 8, 128), bf(n, 2, 128)
+    for bad in ((slab[:2], cap, lens, q, kn, kn, q), (slab, 100, lens, q, kn, kn, q), (slab, cap, few, q, kn, kn, q), (slab, cap, lens, q, kn[:2], kn, q), (slab, cap, lens, q, kn, kn, q[:, :4].contiguous()),
+                (slab, cap, lens, q, None, None, q.float()), (slab, cap, lens, bf(n, 2, 128), kn, kn, q)):
+        _refused(vs.cache8_decode_attn, s, *bad, ws)
+    cache, small, q, k = vs.Cache8(slab[0], cap, 4), vs.Cache8(slab[0], cap + 25, 4), bf(T, 8, 128), bf(T, 2, 128)
+    for bad in ((small, q, k, k, q), (cache, q, k[:5], k, q), (cache, q, k, k.float(), q), (cache, q, k, k, q[:5]), (cache, q, bf(T, 2, 256)[..., :128], k, q)):
+        _refused(vs.cache8_prefill_attn, s, *bad, ws)
+    plan, pos = vs.RotaryPlan(128, (16, 24, 24)), torch.zeros((3, T), dtype=torch.int32)
+    for bad in ((pos, q[:5], k, q, k), (pos, q, k, q, bf(T, 2, 64)), (pos[:, :5], q, k, q, k), (pos[:2], q, k, q, k), (pos, q, k.float(), q, k), (pos, q, None, bf(T, 8, 256)[..., :128], None),
+                (torch.zeros((3, T + 1), dtype=torch.int32), q, k, q, k)):
+        _refused(vs.rotary, s, plan, *bad)
+    for bad in (pos.float(), pos.long()):
+        with pytest.raises(AssertionError):
+            vs.rotary(s, plan, bad, q, k, q, k, stream=0)
+    # and what the library itself refuses still comes from there
+    f32 = _shape(4, 1, 64, vs.VS_F32)
+    with pytest.raises(vs.VSError) as err:
+        vs.cache8_decode_attn(f32, slab, cap, lens, torch.zeros((n, 4, 64)), None, None, torch.zeros((n, 4, 64)), ws, stream=0)
+    assert err.value.code == 3
+    with pytest.raises(vs.VSError) as err:
+        vs.cache8_append(s, slab, cap, lens, bf(n, 41, 2, 128), bf(n, 41, 2, 128), stream=0)
+    assert err.value.code == 4 and list(lens) == [4] * n
