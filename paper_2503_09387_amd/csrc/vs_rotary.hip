@@ -171,6 +171,8 @@ vs_status vs_rotary(const vs_shape* shape, const vs_rotary_plan* plan, const int
     const int64_t head = (int64_t)n_tokens * shape->head_dim * (shape->dtype == VS_F32 ? 4 : 2), nq = p.Hq * head, nk = p.Hkv * head;
     if ((q != q_out && !apart(q, nq, q_out, nq)) || (k != k_out && !apart(k, nk, k_out, nk))) return VS_ERR_SHAPE;
     if (q && k && (!apart(q_out, nq, k_out, nk) || !apart(q_out, nq, k, nk) || !apart(k_out, nk, q, nq))) return VS_ERR_SHAPE;
+    const int64_t np = (int64_t)3 * n_tokens * 4;
+    if ((q && !apart(q_out, nq, positions, np)) || (k && !apart(k_out, nk, positions, np))) return VS_ERR_SHAPE;
     p.q = (const char*)q;
     p.k = (const char*)k;
     p.q_out = (char*)q_out;

@@ -129,6 +129,22 @@ def test_rotary_argument_errors():
         vs.RotaryPlan(128, (16, 24, 23))
 
 
+def test_rotary_refuses_outputs_over_the_positions():
+    """A turned row over positions that other tokens still read.  4 tokens: 28 and 4 heads of 256 bytes, positions of 48."""
+    L, s, plan = vs.lib(), _shape(), vs.RotaryPlan(128, (16, 24, 24)).c
+    q, k, far = FAKE, FAKE + (1 << 20), FAKE + (2 << 20)
+    nq, nk = 4 * 28 * 256, 4 * 4 * 256
+
+    def rot(pos, qo, ko):
+        return L.vs_rotary(ctypes.byref(s), ctypes.byref(plan), pos, 4, q if qo else None, k if ko else None, 0, qo, ko, None)
+
+    for pos in (far, far + nq - 4, far - 44):
+        assert rot(pos, far, k) == 2 and rot(pos, far, None) == 2
+    for pos in (far, far + nk - 4, far - 44):
+        assert rot(pos, q, far) == 2 and rot(pos, None, far) == 2
+    assert rot(q + 64, q, k) == 2 and rot(k + 64, q, k) == 2              # rows turned in place
+
+
 def test_cache8_sizes():
     s = _shape()
     assert vs.cache8_bytes(s, 1) == vs.cache8_bytes(s, 32) == 4 * 8320 and vs.cache8_bytes(s, 33) == 8 * 8320
