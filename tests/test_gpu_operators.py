@@ -879,3 +879,50 @@ def test_decode_with_large_rows_that_nobody_looks_at():
     vs.cache8_decode_attn(sh, slab, cap, lens, q, kn, vn, out, ws)
     for i, n0 in enumerate(lens0):
         check_decode(sh, out, i, q, k, clean, kn, vn, n0, f"stream {i}")
+
+
+@pytest.mark.parametrize("hq,hkv,lens0", [
+    (28, 4, [(131 * i) % 1500 for i in range(64)]),                      # a workgroup for every stream and KV head, nothing shared out
+    (28, 4, [(131 * i) % 1500 for i in range(70)]),                      # and a second launch of few streams, shared out
+    (16, 4, [200 + 37 * i for i in range(39)] + [6000]),                 # shares of a size that is searched for
+    (8, 8, [5500] + [(91 * i) % 300 for i in range(31)]),                # a long one among short ones, nothing shared out
+    (8, 2, [(211 * i) % 900 for i in range(63)] + [2500] + [3000, 40])])  # two launches that are both shared out, over the same counters
+def test_decode_of_many_streams(hq, hkv, lens0):
+    S = len(lens0)
+    sh, slab, cap, lens, k, v, q, kn, vn = decode_case(hq, hkv, lens0, 180)
+    ws = vs.make_cache8_workspace(sh, 0, cap, S, DEV)
+    was, expect = slab.clone(), slab.clone()
+    first = None
+    for turn in range(2):
+        slab.copy_(was)
+        lens, out = lens_array(lens0), torch.full_like(q, float("nan"))
+        vs.cache8_decode_attn(sh, slab, cap, lens, q, kn, vn, out, ws)
+        assert list(lens) == [n + 1 for n in lens0]
+        first = out if first is None else first
+    assert same_bits(first, out)
+    for i in sorted({0, 1, 2, S // 2, 62, 63, 64, 65, S - 3, S - 2, S - 1} & set(range(S))):
+        check_decode(sh, out, i, q, k, v, kn, vn, lens0[i], f"stream {i}")
+    assert torch.isfinite(out.float()).all()
+    vs.cache8_append(sh, expect, cap, lens_array(lens0), kn[:, None].contiguous(), vn[:, None].contiguous())
+    assert same_bits(slab, expect)
+
+
+@pytest.mark.parametrize("at", [3, 4090, 4104, 5000, 8999])
+def test_prefill_finds_a_large_row_anywhere_in_a_long_share(at):
+    """One row of 2^100 among 9000 of 2^-80 that nothing splits: every wavefront walks 70 blocks."""
+    s = AttnShape(28, 4, 128, "bf16")
+    sh, L, T = vs_shape(s), 9000, 600
+    k, v = rows(190, 1, L, 4, 128, loud=False), rows(191, 1, L, 4, 128, loud=False) * 2.0 ** -80
+    v[0, at] *= 2.0 ** 120
+    v[0, at] *= 2.0 ** 60
+    q, kt, vt = rows(192, T, 28, 128, loud=False, sigma=1.0), rows(193, T, 4, 128, loud=False), rows(194, T, 4, 128, loud=False) * 2.0 ** -80
+    slab, lens = slab_of(sh, 1, L), lens_array([0])
+    vs.cache8_append(sh, slab, L, lens, k, v)
+    out = torch.full_like(q, float("nan"))
+    vs.cache8_prefill_attn(sh, vs.Cache8(slab[0], L, L), q, kt, vt, out, vs.make_cache8_workspace(sh, T, L, 0, DEV), first_kept=T)
+    kk, vv = (np.concatenate([ref.stands_for(f64(a[0])), f64(b)]) for a, b in ((k, kt), (v, vt)))
+    for t in (0, T - 1):
+        want, absolute, most = ref.attend(f64(q[t:t + 1]), kk, vv, [L + t + 1], scale32(s))
+        bound = ref.prefill_bound(f64(q[t]), kk[:L + t + 1], vv[:L + t + 1], want[0], absolute[0], most[0], scale32(s))
+        err = off_by(out[t], want[0])
+        assert (err <= bound).all(), f"token {t}: {(err / bound).max():.2f}"
