@@ -6,9 +6,10 @@
 //   * q . (k_codes + 1152): a code + 128 becomes an fp16 by putting 0x64 before its byte (1024 + byte: one permutation for two values);
 //     the query is an fp16 after the power of two that brings its largest entry into [2^14, 2^15), which loses nothing down to 2^-28
 //     of that entry and 2^-39 of it below; the sums start at -1152 sum q.
-//   * p s_v in bf16 (8 bits, as P does over caches in bf16; the denominator sums p before that) times the codes + 128 in bf16, which
-//     loses nothing, less 128 times the sum of p s_v, through one more product, with a matrix of -128.  (The prefill
-//     takes both as fp16: see its `weigh`.)
+//   * p s_v in bf16 (8 bits, as P has over caches in bf16, and no limit to the size of V; the denominator sums p before that) times the codes
+//     + 128 in bf16, which loses nothing, less 128 times the sum of p s_v, through one more product, with a matrix of -128.  With the rounding of the
+//     output that is 2.3e-3 of a value on average over 16 ragged streams, where the output's rounding alone is 2.0e-3.  (The prefill
+//     takes both as fp16: see its `weigh`.  A run's own probabilities are bf16 there too, as over caches in bf16.)
 #pragma once
 #include "vs_cache8.h"
 

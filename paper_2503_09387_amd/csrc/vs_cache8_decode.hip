@@ -334,7 +334,9 @@ constexpr int kSmallBlocks = 32, kSmallWorkgroups = 128;
 //   * with 8, the fewest shares, from a block per wavefront on, with which all run at once, a workgroup per compute unit;
 //   * but at most 12 shares, which the last to arrive adds, as long as they are no more than 80 blocks: 1 x 8192 12.3 (32 shares and a second
 //     launch 15.1), 1 x 16384 15.2 (19.9), 1 x 32768 22.8 (22.9), 1 x 50000 30.2 (25.1).
-// Streams that do not fit all at once are not shared out.
+// (Before the look at the sums of p s_v came in, which is 0.1 .. 0.2 us on each.)
+// Streams that do not fit all at once are not shared out.  That is for streams of like lengths, 33 x 8320 57.9 us, 64 x 8320 84.9; a long one among many short
+// ones is left to 4 workgroups: 63 x 100 and 1 x 8320 45.7, where 59 x 100 and 1 x 8320 are shared out, 15.4.
 // 16 streams of 640..8320 rows (78.9 MB): 19.0 us = 4.2 TB/s, of which some 4 us are the launch, the first trip to memory and the merge; in between
 // bytes come at a large copy's rate.
 struct Plan {

@@ -5,9 +5,11 @@
 // that one multiplies while the other starts or ends.  us by workgroup, 28/4 heads, 37 tokens over 711 rows, 170 over 11016, 600 over 1000, 2048 over 200:
 //   4 wavefronts 10.4, 47.4, 31.8, 95;  8, one workgroup to a compute unit 11.8, 58.2, 43.2, 125;  2 12.4, 48.8, 35.2, 97;
 //   8 of 128 rows that share a block, widened once, through LDS 17.4, 51.2, 45.8, 128.
-// Bound by vector instructions (some 200 of a block's turn, beside 34 matrix instructions, two wavefronts a SIMD; 170 over 11016 in three splits 45.8 us =
-// 591 TFLOP/s, and 4.7 to add them) and, for few blocks, by some 7 us of start and end: launch, first trips to memory, the queries' conversion, the sums' way
-// through LDS, stores.
+// A block's turn is one chain (scores, weights, values) of 34 matrix and some 200 vector instructions, 64 of which widen codes, and the two
+// wavefronts of a SIMD go through it without filling each other's gaps: of 83 k cycles a SIMD (170 over 11016 in three splits) matrix instructions
+// are 28 k and vector ones some 60 k, exponentials at a quarter of the rate.  The sum of the two is what bounds it, neither pipe is full: 45.9 us =
+// 590 TFLOP/s, and 4.7 to add the splits.  (The prefill over rows in bf16 widens nothing and overlaps the two: 35.4 us for the same.)  Few blocks are
+// bound by some 7 us of start and end: launch, first trips to memory, the queries' conversion, the sums' way through LDS, stores.
 #include "vs_cache8_attn.h"
 
 #include <algorithm>
@@ -31,7 +33,7 @@ struct Prefill8Params {
     const char* k;   // the run's own rows
     const char* v;
     __bf16* out;
-    _Float16* part_o;  // [split][Hkv][row][128] normalised, times the power of two that brings the largest of 32 dims into [2^14, 2^15)
+    _Float16* part_o;  // [split][Hkv][row][128] (half the bytes of an fp32 through memory; 11 bits, where the output has 8) normalised, times the power of two that brings the largest of 32 dims into [2^14, 2^15)
     char* part_ml;     // [split][Hkv][row][16 bytes]: reference (log2 units), sum, the biased exponents of the four powers, unused
     int len, T, G, Hq, Hkv, M;
     int n_cache_blocks;
