@@ -171,17 +171,17 @@ def _check(rc, what):
         raise VSError(rc, what)
 
 
-def _dense(t, n_bytes, what):
-    """The address of a tensor (or None) that has to be n_bytes, one behind the other."""
+def _dense(t, n_bytes, what, size=0):
+    """The address of a tensor (or None) that has to be n_bytes, one behind the other; or to begin with them, if its elements are of `size`."""
     if t is None:
         return None
-    if t.nbytes == n_bytes and t.is_contiguous():
+    if (t.nbytes == n_bytes or t.nbytes > n_bytes and t.element_size() == size) and t.is_contiguous():
         return t.data_ptr()
     raise VSError(2, f"{what}: a tensor of {tuple(t.shape)} {t.dtype} where {n_bytes} bytes in a row belong")
 
 
-def _head_bytes(shape):
-    return shape.head_dim * 4 if shape.dtype == VS_F32 else shape.head_dim * 2
+def _element_size(shape):
+    return 4 if shape.dtype == VS_F32 else 2
 
 
 def workspace_bytes(shape, max_q_tokens, max_cache_rows, n_streams):
@@ -417,10 +417,11 @@ def rotary(shape, plan, positions, q, k, q_out, k_out, inverse=False, stream=Non
     """positions: device int32 [3][T]; q, q_out [T][Hq][D], k, k_out [T][Hkv][D] (either pair may be None; in place: out is in)."""
     assert positions.element_size() == 4 and not positions.is_floating_point()
     what, n = "vs_rotary", positions.shape[1]
-    head = n * _head_bytes(shape)
-    nq, nk = shape.n_q_heads * head, shape.n_kv_heads * head
-    _check(lib().vs_rotary(ctypes.byref(shape), ctypes.byref(plan.c), _dense(positions, 12 * n, what), n, _dense(q, nq, what), _dense(k, nk, what),
-                           bool(inverse), _dense(q_out, nq, what), _dense(k_out, nk, what), _stream(stream)), what)
+    size = _element_size(shape)
+    head = n * shape.head_dim * size
+    nq, nk = head * shape.n_q_heads, head * shape.n_kv_heads
+    _check(lib().vs_rotary(ctypes.byref(shape), ctypes.byref(plan.c), _dense(positions, 12 * n, what, 4), n, _dense(q, nq, what, size), _dense(k, nk, what, size),
+                           bool(inverse), _dense(q_out, nq, what, size), _dense(k_out, nk, what, size), _stream(stream)), what)
 
 
 class _CCache8(ctypes.Structure):
@@ -440,7 +441,7 @@ def _caches8(shape, n, slab, capacity, lens, what):
     """The address of n caches of that capacity, which have to be in the tensor, with as many lengths."""
     if slab.nbytes < n * _cache8_size(shape.n_kv_heads, capacity) or not slab.is_contiguous():
         raise VSError(2, f"{what}: {slab.nbytes} bytes where {n} caches of {capacity} rows belong")
-    if len(lens) < n:
+    if isinstance(lens, ctypes.Array) and len(lens) < n:
         raise VSError(2, f"{what}: {len(lens)} lengths for {n} caches")
     return slab.data_ptr()
 
@@ -486,7 +487,7 @@ def cache8_append(shape, slab, capacity, lens, k_rows, v_rows, first_kept=0, str
     """slab: uint8 [n_caches][cache8_bytes]; lens: ctypes int32 array [n_caches] (host), grown by the rows kept;
     k_rows, v_rows [n_caches][T][Hkv][D], rows first_kept.. of which are quantised into the caches."""
     what, n, tokens = "vs_cache8_append", k_rows.shape[0], k_rows.shape[1]
-    nk = n * tokens * shape.n_kv_heads * _head_bytes(shape)
+    nk = n * tokens * shape.n_kv_heads * shape.head_dim * _element_size(shape)
     _check(lib().vs_cache8_append(ctypes.byref(shape), n, _caches8(shape, n, slab, capacity, lens, what), capacity, lens, _dense(k_rows, nk, what),
                                   _dense(v_rows, nk, what), tokens, first_kept, _stream(stream)), what)
 
@@ -494,8 +495,8 @@ def cache8_append(shape, slab, capacity, lens, k_rows, v_rows, first_kept=0, str
 def cache8_read(shape, slab, capacity, lens, first_rows, k_out, v_out, stream=None):
     """Rows first_rows[i].. (None: 0..) of every cache as what they stand for -> k_out, v_out [n_caches][n][Hkv][D]."""
     what, n, rows = "vs_cache8_read", k_out.shape[0], k_out.shape[1]
-    nk = n * rows * shape.n_kv_heads * _head_bytes(shape)
-    if first_rows is not None and len(first_rows) < n:
+    nk = n * rows * shape.n_kv_heads * shape.head_dim * _element_size(shape)
+    if isinstance(first_rows, ctypes.Array) and len(first_rows) < n:
         raise VSError(2, f"{what}: {len(first_rows)} first rows for {n} caches")
     _check(lib().vs_cache8_read(ctypes.byref(shape), n, _caches8(shape, n, slab, capacity, lens, what), capacity, lens, first_rows, rows,
                                 _dense(k_out, nk, what), _dense(v_out, nk, what), _stream(stream)), what)
@@ -504,23 +505,25 @@ def cache8_read(shape, slab, capacity, lens, first_rows, k_out, v_out, stream=No
 def cache8_decode_attn(shape, slab, capacity, lens, q, k_new, v_new, out, workspace, stream=None):
     """decode_attn over a slab of caches in 8 bits; q, out [n_streams][Hq][D]."""
     what, n = "vs_cache8_decode_attn", q.shape[0]
-    head = n * _head_bytes(shape)
-    nq, nk = shape.n_q_heads * head, shape.n_kv_heads * head
+    size = _element_size(shape)
+    head = n * shape.head_dim * size
+    nq, nk = head * shape.n_q_heads, head * shape.n_kv_heads
     wp, wb = _ws(workspace)
-    _check(lib().vs_cache8_decode_attn(ctypes.byref(shape), n, _caches8(shape, n, slab, capacity, lens, what), capacity, lens, _dense(q, nq, what),
-                                       _dense(k_new, nk, what), _dense(v_new, nk, what), _dense(out, nq, what), wp, wb, _stream(stream)), what)
+    _check(lib().vs_cache8_decode_attn(ctypes.byref(shape), n, _caches8(shape, n, slab, capacity, lens, what), capacity, lens, _dense(q, nq, what, size),
+                                       _dense(k_new, nk, what, size), _dense(v_new, nk, what, size), _dense(out, nq, what, size), wp, wb, _stream(stream)), what)
 
 
 def cache8_prefill_attn(shape, cache, q, k_t, v_t, out, workspace, first_kept=None, stream=None):
     """A run's tokens over a Cache8; rows first_kept.. of the run (None: the last, the carrier) are quantised into it."""
     what, n = "vs_cache8_prefill_attn", q.shape[0]
-    head = n * _head_bytes(shape)
-    nq, nk = shape.n_q_heads * head, shape.n_kv_heads * head
+    size = _element_size(shape)
+    head = n * shape.head_dim * size
+    nq, nk = head * shape.n_q_heads, head * shape.n_kv_heads
     if cache.data.nbytes < _cache8_size(shape.n_kv_heads, cache.c.capacity):
         raise VSError(2, f"{what}: {cache.data.nbytes} bytes where a cache of {cache.c.capacity} rows belongs")
     wp, wb = _ws(workspace)
-    _check(lib().vs_cache8_prefill_attn(ctypes.byref(shape), ctypes.byref(cache.c), _dense(q, nq, what), _dense(k_t, nk, what), _dense(v_t, nk, what), n,
-                                        n - 1 if first_kept is None else first_kept, _dense(out, nq, what), wp, wb, _stream(stream)), what)
+    _check(lib().vs_cache8_prefill_attn(ctypes.byref(shape), ctypes.byref(cache.c), _dense(q, nq, what, size), _dense(k_t, nk, what, size), _dense(v_t, nk, what, size), n,
+                                        n - 1 if first_kept is None else first_kept, _dense(out, nq, what, size), wp, wb, _stream(stream)), what)
 
 
 def carrier_mean_pool(e, c_out, dtype, stream=None):

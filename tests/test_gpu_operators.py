@@ -926,3 +926,24 @@ def test_prefill_finds_a_large_row_anywhere_in_a_long_share(at):
         bound = ref.prefill_bound(f64(q[t]), kk[:L + t + 1], vv[:L + t + 1], want[0], absolute[0], most[0], scale32(s))
         err = off_by(out[t], want[0])
         assert (err <= bound).all(), f"token {t}: {(err / bound).max():.2f}"
+
+
+def test_the_first_tokens_of_larger_buffers():
+    """Tensors that go on behind the run's tokens: the same bits in front, nothing written behind.  Lengths through a pointer, as through an array."""
+    sh, T, L, cap = vs.Shape.make(8, 2, 128, "bf16"), 11, 100, 130
+    q, k, v = rows(200, 20, 8, 128, loud=False), rows(201, 20, 2, 128, loud=False), rows(202, 20, 2, 128, loud=False)
+    pos = torch.arange(3 * T, device=DEV, dtype=torch.int32).view(3, T)
+    plan, slab, lens = vs.RotaryPlan(128, (16, 24, 24)), slab_of(sh, 1, cap), lens_array([0])
+    vs.cache8_append(sh, slab, cap, ctypes.cast(lens, ctypes.POINTER(ctypes.c_int32)), rows(203, 1, L, 2, 128), rows(204, 1, L, 2, 128))
+    assert lens[0] == L
+    ws = vs.make_cache8_workspace(sh, T, cap, 1, DEV)
+    qo, ko, out, step = torch.full_like(q, 7.0), torch.full_like(k, 7.0), torch.full_like(q, 7.0), torch.full_like(q, 7.0)
+    exact = [torch.empty_like(t[:T]) for t in (q, k, q)] + [torch.empty_like(q[:1])]
+    vs.rotary(sh, plan, pos, q, k, qo, ko)
+    vs.rotary(sh, plan, pos, q[:T], k[:T], exact[0], exact[1])
+    vs.cache8_prefill_attn(sh, vs.Cache8(slab[0], cap, L), q[:T], k, v, out, ws, first_kept=T)
+    vs.cache8_prefill_attn(sh, vs.Cache8(slab[0], cap, L), q[:T], k[:T], v[:T], exact[2], ws, first_kept=T)
+    vs.cache8_decode_attn(sh, slab, cap, lens_array([L]), q[:1], k, v, step, ws)
+    vs.cache8_decode_attn(sh, slab, cap, lens_array([L]), q[:1], k[:1], v[:1], exact[3], ws)
+    for got, want, n in zip((qo, ko, out, step), exact, (T, T, T, 1)):
+        assert same_bits(got[:n], want) and (got[n:] == 7.0).all()

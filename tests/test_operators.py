@@ -290,6 +290,7 @@ def test_binding_refuses_tensors_that_are_not_what_the_call_covers():
     for bad in ((pos, q[:5], k, q, k), (pos, q, k, q, bf(T, 2, 64)), (pos[:, :5], q, k, q, k), (pos[:2], q, k, q, k), (pos, q, k.float(), q, k), (pos, q, None, bf(T, 8, 256)[..., :128], None),
                 (torch.zeros((3, T + 1), dtype=torch.int32), q, k, q, k)):
         _refused(vs.rotary, s, plan, *bad)
+    _refused(vs.cache8_append, s, slab, cap, lens, bf(n, T, 2, 128), bf(n, T + 1, 2, 128))       # caches that begin elsewhere in one of the two
     for bad in (pos.float(), pos.long()):
         with pytest.raises(AssertionError):
             vs.rotary(s, plan, bad, q, k, q, k, stream=0)
